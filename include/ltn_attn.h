@@ -329,6 +329,101 @@ ltn_status ltn_attn_decode_steps_dkdv(const void* q, const void* k, const void* 
                                       int Bt, int H, int S, int Dk, int Dv,
                                       ltn_dtype dtype, void* stream);
 
+/*
+ * Gated delta rule: the recurrence above with a state that is corrected before it is added to.  Per head,
+ *
+ *     A_t = exp(g_t) S_{t-1},   u_t = beta_t (v_t - A_t^T k_t),   S_t = A_t + k_t u_t^T,   o_t = scale S_t^T q_t,
+ *
+ * evaluated in chunks of 64 tokens (products of matrices, and one triangular inverse a chunk); S as everywhere here, fp32
+ * [.., Dk, Dv] with row = key feature.  Log decays and beta are per token and head.
+ *
+ *   q, k     in : device, [Bt,Hk,N,Dk] dtype; value head h reads key head h / (H / Hk), H a multiple of Hk
+ *   v        in : device, [Bt,H,N,Dv] dtype                 o       out: device, [Bt,H,N,Dv] dtype
+ *   g, beta  in : device, [Bt,H,N] fp32; g <= 0 (-inf: the state is dropped), beta usually in [0,1].  Values are not
+ *                 read on the host.  The keys' norms are the caller's affair: sqrt(beta) |k| <= 1 keeps the recurrence stable
+ *   kv_in    in : device, [Bt,H,Dk,Dv] fp32, or NULL (zero)  kv_out  out: the same, or NULL; may be kv_in
+ *   cu       in : NULL, or packed sequences: device, seqs + 1 int32 values in ascending order within [0, N].  Sequence i is
+ *                 tokens cu[i] .. cu[i+1] - 1 of the one row (Bt must be 1); it may be empty.  States are then
+ *                 [seqs,H,Dk,Dv].  Tokens outside cu[0] .. cu[seqs] - 1 are not read, and what the outputs hold there is left
+ *                 as it was.  Values are not read on the host; whatever they are, no access leaves the tensors (sequences
+ *                 that they make overlap have undefined results).  seqs is not used without cu
+ *   workspace   : device scratch of ltn_delta_workspace_bytes(..., call = 0) bytes
+ * (Dk, Dv) in {64,128} x {64,128}; N < 2^31 - 64.  fp32 tensors: fp32 arithmetic throughout.  bf16 tensors: bf16 matrix
+ * products with fp32 sums; what enters the state enters in two bf16 parts, so that kv_out is exact to about 4e-6 of
+ * its norm, not to a bf16 rounding; o is rounded to bf16.  An infinity or NaN in a token reaches the later tokens of its
+ * sequence, and may reach the other tokens of its chunk of 64.
+ * N == 0 (or an empty sequence) hands kv_in (or zeros) on to kv_out.
+ */
+ltn_status ltn_delta_fwd(const void* q, const void* k, const void* v, void* o, const float* g, const float* beta,
+                         const int* cu, const float* kv_in, float* kv_out, float scale,
+                         int Bt, int Hk, int H, long long N, int Dk, int Dv, int seqs, ltn_dtype dtype,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradients, from the same inputs and d_o alone (nothing saved by the forward), zero initial state:
+ *
+ *   d_o        in : device, [Bt,H,N,Dv] dtype
+ *   dq, dk    out : device, [Bt,Hk,N,Dk] dtype, summed over the value heads that share a key head in a fixed order
+ *   dv        out : device, [Bt,H,N,Dv] dtype
+ *   dg, dbeta out : device, [Bt,H,N] dtype (the tensors' type: with bf16 tensors they are sums of bf16 products, and as exact)
+ *   workspace     : device scratch of ltn_delta_workspace_bytes(..., call = 1) bytes; per 64 tokens and value head it holds,
+ *                   among others, the state before them and its derivative behind them (7B-shaped layer: 2.2 GB)
+ * Other arguments, packed sequences and shapes as above.
+ */
+ltn_status ltn_delta_bwd(const void* q, const void* k, const void* v, const void* d_o,
+                         void* dq, void* dk, void* dv, void* dg, void* dbeta, const float* g, const float* beta,
+                         const int* cu, float scale, int Bt, int Hk, int H, long long N, int Dk, int Dv, int seqs,
+                         ltn_dtype dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Scratch bytes of ltn_delta_fwd (call = 0) and ltn_delta_bwd (1); seqs = 0: no packed sequences.  0 for what they refuse. */
+size_t ltn_delta_workspace_bytes(int Bt, int H, long long N, int Dk, int Dv, int seqs, ltn_dtype dtype, int call);
+
+/*
+ * S steps of the recurrence against running states, in one call (S = 1: one token of every sequence):
+ *
+ *   q, k in : device, [Bt,Hk,S,Dk] dtype     v in, o out : device, [Bt,H,S,Dv] dtype     g, beta in : device, [Bt,H,S] fp32
+ *   kv in/out : device, [Bt,H,Dk,Dv] fp32
+ * fp32 arithmetic whatever dtype is; bit for bit the result of S single-token calls.
+ */
+ltn_status ltn_delta_decode_steps(const void* q, const void* k, const void* v, void* o, float* kv,
+                                  const float* g, const float* beta, float scale,
+                                  int Bt, int Hk, int H, int S, int Dk, int Dv, ltn_dtype dtype, void* stream);
+
+/*
+ * What stands between two blocks of a layer stack, on rows of C features: the norm behind a block, its gate, the residual
+ * scale and sum, the norm before the next block (SimpleRMSNorm, Sec. 3.1.3, or with weights the usual RMS norm):
+ *
+ *     n = y / sqrt(mean(y^2) + eps)  (after == 0: n = y)       x_out = x + scale gate (.) n (.) w_after
+ *     h = x_out / sqrt(mean(x_out^2) + eps) (.) w_before       (of x_out as it is before it is rounded)
+ *
+ *   x, y     in : device, [rows, C] dtype (the residual stream, the block's output)
+ *   gate     in : device, [gates, C] dtype, or NULL (ones): row r reads gate r / (rows / gates); rows a multiple of gates.
+ *                 gates = rows: element by element, Bt: one for each sequence, 1: one for all
+ *   w_after, w_before in : device, [C] fp32, or NULL (ones)
+ *   x_out, h out: device, [rows, C] dtype; x_out may be x itself
+ * C a multiple of 8, at most 8192; fp32 arithmetic for either dtype.  eps as for ltn_gate_fwd.
+ */
+ltn_status ltn_block_norm_fwd(const void* x, const void* y, const void* gate, const float* w_after, const float* w_before,
+                              void* x_out, void* h, float scale, float eps, int after,
+                              long long rows, long long gates, int C, ltn_dtype dtype, void* stream);
+
+/*
+ * Its gradients, from the forward's inputs (x as it was before) and:
+ *
+ *   d_x_out  in : device, [rows, C] dtype, or NULL (zero)     d_h in : device, [rows, C] dtype
+ *   d_x, d_y out: device, [rows, C] dtype     d_gate out: device, [gates, C] dtype, NULL exactly when gate is
+ *   d_w_after, d_w_before out: device, [C] fp32, NULL exactly when the weight is
+ *   workspace   : device scratch of ltn_block_norm_workspace_bytes(...) bytes (sums over rows go through it in a fixed order)
+ * With rows == 0 the gradients of the weights and of the gates are zero.
+ */
+ltn_status ltn_block_norm_bwd(const void* x, const void* y, const void* gate, const float* w_after, const float* w_before,
+                              const void* d_x_out, const void* d_h, void* d_x, void* d_y, void* d_gate,
+                              float* d_w_after, float* d_w_before, float scale, float eps, int after,
+                              long long rows, long long gates, int C, ltn_dtype dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+size_t ltn_block_norm_workspace_bytes(long long rows, int C);
+
 /* Block length the library uses for (D, dtype) when `block` is 0; 0 if unsupported.
  * The paper leaves the block sizes B_r, B_c of its tiling as inputs (App. B, Algorithms 3
  * and 4); the result does not depend on them beyond rounding.  bf16: 64 for every D (a

@@ -27,6 +27,8 @@ SYMBOLS = (
     "ltn_prologue_fwd", "ltn_prologue_bwd", "ltn_prologue_workspace_bytes",
     "ltn_attn_fwd_dkdv", "ltn_attn_bwd_dkdv", "ltn_attn_decode_steps_dkdv",
     "ltn_attn_query_plan", "ltn_attn_query_cut", "ltn_attn_query_sweeps", "ltn_attn_set_debug_plan", "ltn_attn_fwd_static", "ltn_attn_bwd_tiled", "ltn_probe_stream_read", "ltn_attn_workspace_bytes_dkdv",
+    "ltn_delta_fwd", "ltn_delta_bwd", "ltn_delta_decode_steps", "ltn_delta_workspace_bytes",
+    "ltn_block_norm_fwd", "ltn_block_norm_bwd", "ltn_block_norm_workspace_bytes",
 )
 
 
@@ -105,6 +107,20 @@ def load_library():
     lib.ltn_attn_query_sweeps.restype = ci
     lib.ltn_attn_set_debug_plan.argtypes = [ci, ci]
     lib.ltn_attn_set_debug_plan.restype = ci
+    lib.ltn_delta_fwd.argtypes = [vp, vp, vp, vp, fp, fp, vp, fp, fp, cf, ci, ci, ci, cl, ci, ci, ci, ci, vp, sz, vp]
+    lib.ltn_delta_fwd.restype = ci
+    lib.ltn_delta_bwd.argtypes = [vp] * 9 + [fp, fp, vp, cf, ci, ci, ci, cl, ci, ci, ci, ci, vp, sz, vp]
+    lib.ltn_delta_bwd.restype = ci
+    lib.ltn_delta_decode_steps.argtypes = [vp, vp, vp, vp, fp, fp, fp, cf, ci, ci, ci, ci, ci, ci, ci, vp]
+    lib.ltn_delta_decode_steps.restype = ci
+    lib.ltn_delta_workspace_bytes.argtypes = [ci, ci, cl, ci, ci, ci, ci, ci]
+    lib.ltn_delta_workspace_bytes.restype = sz
+    lib.ltn_block_norm_fwd.argtypes = [vp, vp, vp, fp, fp, vp, vp, cf, cf, ci, cl, cl, ci, ci, vp]
+    lib.ltn_block_norm_fwd.restype = ci
+    lib.ltn_block_norm_bwd.argtypes = [vp, vp, vp, fp, fp, vp, vp, vp, vp, vp, fp, fp, cf, cf, ci, cl, cl, ci, ci, vp, sz, vp]
+    lib.ltn_block_norm_bwd.restype = ci
+    lib.ltn_block_norm_workspace_bytes.argtypes = [cl, ci]
+    lib.ltn_block_norm_workspace_bytes.restype = sz
     _bind_native(lib)
     _lib = lib
     return lib
@@ -660,3 +676,163 @@ def ltn_attn_decode_steps_dkdv(q, k, v, kv, decay, out=None):
     if rc != 0:
         raise LtnError(rc, "ltn_attn_decode_steps_dkdv")
     return o
+
+
+def ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, dtype, call) -> int:
+    """call: 0 = ltn_delta_fwd, 1 = ltn_delta_bwd; seqs: packed sequences, 0 without."""
+    return int(load_library().ltn_delta_workspace_bytes(int(Bt), int(H), int(N), int(Dk), int(Dv), int(seqs),
+                                                        _dtype_code(dtype), int(call)))
+
+
+def _check_delta(q, k, v, g, beta, cu):
+    """(Bt, Hk, H, N, Dk, Dv, packed sequences or 0, rows of states)."""
+    _devs("q k v g beta", q, k, v, g, beta)
+    if q.dim() != 4 or q.shape != k.shape or v.dim() != 4 or v.shape[0] != q.shape[0] or v.shape[2] != q.shape[2]:
+        raise ValueError("q, k must be [Bt,Hk,N,Dk] and v [Bt,H,N,Dv]")
+    if not (q.dtype == k.dtype == v.dtype):
+        raise ValueError("q, k, v must share a dtype")
+    Bt, Hk, N, Dk = q.shape
+    H, Dv = v.shape[1], v.shape[3]
+    if H and (Hk == 0 or H % Hk):
+        raise ValueError("the heads of v must be a multiple of those of q and k")
+    for t, n in ((g, "g"), (beta, "beta")):
+        if t.dtype != torch.float32 or tuple(t.shape) != (Bt, H, N):
+            raise ValueError(f"{n} must be fp32 [Bt,H,N]")
+    if cu is None:
+        seqs, rows = 0, Bt
+    else:
+        _dev(cu, "cu")
+        if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 2 or Bt != 1:
+            raise ValueError("cu must be int32 [seqs + 1] over tensors with Bt = 1")
+        seqs = rows = cu.numel() - 1
+    if any(t.device != q.device for t in (k, v, g, beta) + (() if cu is None else (cu,))):
+        raise ValueError("all tensors must live on one GPU")
+    return Bt, Hk, H, N, Dk, Dv, seqs, rows
+
+
+def ltn_delta_fwd(q, k, v, g, beta, kv_in=None, cu=None, scale=1.0, return_state=False, out=None, kv_out=None):
+    """Gated delta rule: S_t = exp(g_t) S_{t-1} corrected by beta_t k_t (v_t - ..)^T, o_t = scale S_t^T q_t, optionally continuing
+    from / returning the fp32 states [rows,H,Dk,Dv].  cu: ends of packed sequences (int32, on the GPU, Bt = 1)."""
+    lib = load_library()
+    Bt, Hk, H, N, Dk, Dv, seqs, rows = _check_delta(q, k, v, g, beta, cu)
+    o = torch.empty_like(v) if out is None else _out(out, "out", v.numel(), v.dtype)
+    if kv_in is not None:
+        _dev(kv_in, "kv_in")
+        if kv_in.dtype != torch.float32 or tuple(kv_in.shape) != (rows, H, Dk, Dv):
+            raise ValueError("kv_in must be fp32 [Bt,H,Dk,Dv] ([seqs,H,Dk,Dv] with cu)")
+    if kv_out is not None:
+        _out(kv_out, "kv_out", rows * H * Dk * Dv, torch.float32)
+    elif return_state:
+        kv_out = torch.empty((rows, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    code = _dtype_code(q.dtype)
+    ws_bytes = int(lib.ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, code, 0))
+    ws = _workspace(ws_bytes, q.device)
+    rc = _call(lib.ltn_delta_fwd, q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(g), _ptr(beta), _ptr(cu), _ptr(kv_in),
+               _ptr(kv_out), float(scale), Bt, Hk, H, N, Dk, Dv, seqs, code, _ptr(ws), ws_bytes)
+    if rc != 0:
+        raise LtnError(rc, "ltn_delta_fwd")
+    return (o, kv_out) if (return_state or kv_out is not None) else o
+
+
+def ltn_delta_bwd(q, k, v, g, beta, d_o, cu=None, scale=1.0, out=None):
+    """(dq, dk, dv, dg, dbeta) of ltn_delta_fwd from zero initial states, all in q's dtype."""
+    lib = load_library()
+    Bt, Hk, H, N, Dk, Dv, seqs, _ = _check_delta(q, k, v, g, beta, cu)
+    _dev(d_o, "d_o")
+    if d_o.shape != v.shape or d_o.dtype != v.dtype or d_o.device != q.device:
+        raise ValueError("d_o must have v's shape, dtype and device")
+    if out is None:
+        dg = torch.empty((Bt, H, N), dtype=q.dtype, device=q.device)
+        dq, dk, dv, dg, dbeta = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), dg, torch.empty_like(dg)
+    else:
+        dq, dk, dv, dg, dbeta = (_out(t, "out", n, q.dtype) for t, n in zip(out, (q.numel(), k.numel(), v.numel(), g.numel(), g.numel())))
+    code = _dtype_code(q.dtype)
+    ws_bytes = int(lib.ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, code, 1))
+    ws = _workspace(ws_bytes, q.device)
+    rc = _call(lib.ltn_delta_bwd, q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg),
+               _ptr(dbeta), _ptr(g), _ptr(beta), _ptr(cu), float(scale), Bt, Hk, H, N, Dk, Dv, seqs, code, _ptr(ws), ws_bytes)
+    if rc != 0:
+        raise LtnError(rc, "ltn_delta_bwd")
+    return dq, dk, dv, dg, dbeta
+
+
+def ltn_delta_decode_steps(q, k, v, kv, g, beta, scale=1.0, out=None):
+    """S steps of the gated delta rule: q, k [Bt,Hk,S,Dk]; v [Bt,H,S,Dv]; kv fp32 [Bt,H,Dk,Dv] updated in place; returns o."""
+    lib = load_library()
+    Bt, Hk, H, S, Dk, Dv, _, _ = _check_delta(q, k, v, g, beta, None)
+    _dev(kv, "kv")
+    if kv.dtype != torch.float32 or tuple(kv.shape) != (Bt, H, Dk, Dv) or kv.device != q.device:
+        raise ValueError("kv must be fp32 [Bt,H,Dk,Dv] on q's device")
+    o = torch.empty_like(v) if out is None else _out(out, "out", v.numel(), v.dtype)
+    rc = _call(lib.ltn_delta_decode_steps, q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(kv), _ptr(g), _ptr(beta),
+               float(scale), Bt, Hk, H, S, Dk, Dv, _dtype_code(q.dtype))
+    if rc != 0:
+        raise LtnError(rc, "ltn_delta_decode_steps")
+    return o
+
+
+def ltn_block_norm_workspace_bytes(rows, C) -> int:
+    return int(load_library().ltn_block_norm_workspace_bytes(int(rows), int(C)))
+
+
+def _check_block_norm(x, y, gate, w_after, w_before, after, others=()):
+    """(rows, gates, C); `others`: (name, tensor) of x's shape and dtype."""
+    rows, C = _rows(x, "x")
+    for n, t in (("y", y), *others):
+        _dev(t, n)
+        if t.shape != x.shape or t.dtype != x.dtype:
+            raise ValueError(f"{n} must have x's shape and dtype")
+    for n, t in (("w_after", w_after), ("w_before", w_before)):
+        if t is not None:
+            _dev(t, n)
+            if t.dtype != torch.float32 or tuple(t.shape) != (C,):
+                raise ValueError(f"{n} must be fp32 [C]")
+    if w_after is not None and not after:
+        raise ValueError("w_after belongs to the norm behind the block, which after=False leaves out")
+    gates = 0
+    if gate is not None:
+        _dev(gate, "gate")
+        if gate.dtype != x.dtype or gate.dim() < 1 or gate.shape[-1] != C:
+            raise ValueError("gate must be [gates, C] in x's dtype")
+        gates = 1
+        for n in gate.shape[:-1]:
+            gates *= n
+        if gates == 0 or rows % gates:
+            raise ValueError("the rows of x must be a multiple of those of gate")
+    if any(t is not None and t.device != x.device for t in (y, gate, w_after, w_before, *(t for _, t in others))):
+        raise ValueError("all tensors must live on one GPU")
+    return rows, gates, C
+
+
+def ltn_block_norm_fwd(x, y, gate=None, w_after=None, w_before=None, scale=1.0, eps=0.0, after=True, out=None):
+    """(x_out, h): x_out = x + scale gate (.) norm(y) (.) w_after, h = norm(x_out) (.) w_before over the last axis, with
+    norm(t) = t / sqrt(mean(t^2) + eps) (after=False: y itself).  gate: [.., C] whose rows each serve as many of x's."""
+    lib = load_library()
+    rows, gates, C = _check_block_norm(x, y, gate, w_after, w_before, after)
+    if out is None:
+        xo, h = torch.empty_like(x), torch.empty_like(x)
+    else:
+        xo, h = (_out(t, "out", x.numel(), x.dtype) for t in out)
+    rc = _call(lib.ltn_block_norm_fwd, x.device, _ptr(x), _ptr(y), _ptr(gate), _ptr(w_after), _ptr(w_before), _ptr(xo), _ptr(h),
+               float(scale), float(eps), int(bool(after)), rows, gates, C, _dtype_code(x.dtype))
+    if rc != 0:
+        raise LtnError(rc, "ltn_block_norm_fwd")
+    return xo, h
+
+
+def ltn_block_norm_bwd(x, y, d_x_out, d_h, gate=None, w_after=None, w_before=None, scale=1.0, eps=0.0, after=True):
+    """(d_x, d_y, d_gate, d_w_after, d_w_before) of ltn_block_norm_fwd from its inputs; None in the place of what it had none
+    of.  d_x_out: the gradient by x_out, or None (zero)."""
+    lib = load_library()
+    others = [("d_h", d_h)] + ([] if d_x_out is None else [("d_x_out", d_x_out)])
+    rows, gates, C = _check_block_norm(x, y, gate, w_after, w_before, after, others)
+    dx, dy = torch.empty_like(x), torch.empty_like(x)
+    dgate, dwa, dwb = (None if t is None else torch.empty_like(t) for t in (gate, w_after, w_before))
+    ws_bytes = int(lib.ltn_block_norm_workspace_bytes(rows, C))
+    ws = _workspace(ws_bytes, x.device)
+    rc = _call(lib.ltn_block_norm_bwd, x.device, _ptr(x), _ptr(y), _ptr(gate), _ptr(w_after), _ptr(w_before), _ptr(d_x_out),
+               _ptr(d_h), _ptr(dx), _ptr(dy), _ptr(dgate), _ptr(dwa), _ptr(dwb), float(scale), float(eps), int(bool(after)),
+               rows, gates, C, _dtype_code(x.dtype), _ptr(ws), ws_bytes)
+    if rc != 0:
+        raise LtnError(rc, "ltn_block_norm_bwd")
+    return dx, dy, dgate, dwa, dwb

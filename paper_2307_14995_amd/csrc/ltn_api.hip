@@ -2,6 +2,7 @@
 // before any launch), choice of block length and value-column split, and dispatch
 // to the gfx950 kernels.  See include/ltn_attn.h for the contract.
 #include "../../include/ltn_attn.h"
+#include "ltn_args.h"
 #include "ltn_kernels.h"
 
 #include <atomic>
@@ -10,35 +11,9 @@
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // Test-only overrides of the launch plan (ltn_attn_set_debug_plan); 0 = the library's choice.
 std::atomic<int> g_debug_dv{0};
 std::atomic<int> g_debug_segs{0};
-
-// A tensor argument as a byte range.  Outputs are written while inputs are still being
-// read (tile loads run up to three blocks ahead of the stores), so any overlap between an
-// output and an input, or between two outputs, is rejected, not only equal base pointers.
-struct Span { const void* p; size_t bytes; };
-
-bool spans_overlap(const Span& a, const Span& b) {
-    if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return false;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-    return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
-}
-
-// true when some output overlaps an input or another output
-bool outputs_alias(const Span* outs, int n_out, const Span* ins, int n_in) {
-    for (int a = 0; a < n_out; ++a) {
-        for (int b = 0; b < n_in; ++b)
-            if (spans_overlap(outs[a], ins[b])) return true;
-        for (int b = a + 1; b < n_out; ++b)
-            if (spans_overlap(outs[a], outs[b])) return true;
-    }
-    return false;
-}
-
-size_t esize_of(ltn_dtype dtype) { return dtype == LTN_BF16 ? 2 : 4; }
 
 // Value columns handled per workgroup.  Every value-column slice of a chain recomputes
 // that chain's score tiles and re-reads its first two operands through L2, and a compute

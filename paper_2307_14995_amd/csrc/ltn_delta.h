@@ -1,0 +1,197 @@
+// Gated delta rule: what its kernels and the C-ABI layer share.  Internal; the public boundary is include/ltn_attn.h.
+//
+// One head, one sequence, state S [Dk x Dv] (fp32, row = key feature, column = value feature):
+//
+//     S_t = a_t S_{t-1} + k_t u_t^T,   u_t = beta_t z_t,   z_t = v_t - a_t S_{t-1}^T k_t,   o_t = scale S_t^T q_t,   a_t = exp(g_t)
+//
+// In chunks of 64 tokens, with S0 the state before a chunk, G the log decays summed from its first token on,
+// gam = exp(G), end = exp(G_last - G) and R[r,i] = exp(G_r - G_i) for r >= i, else 0 (only exponents of sums of log
+// decays between two tokens are formed, never a quotient of products):
+//
+//     L = strict lower triangle of R (.) K K^T      T' = (I + L diag(beta))^-1      P = scale R (.) Q K^T
+//     X = V - diag(gam) K S0      Z = T' X      U = diag(beta) Z
+//     O = scale diag(gam) Q S0 + P U      S1 = gam_last S0 + K^T diag(end) U
+//
+// and, with dS the derivative by S1 and T = (I + diag(beta) L)^-1,
+//
+//     dU = P^T dO + diag(end) K dS      dY = T^T dU      dV = diag(beta) dY      dbeta = rows of dY (.) Z
+//     dS0 = gam_last dS + Q^T diag(scale gam) dO - K^T diag(gam) dV
+//     dP = scale R (.) dO U^T      E = -R (.) diag(beta) dY U^T below the diagonal
+//     dQ = scale diag(gam) dO S0^T + dP K
+//     dK = -diag(gam) dV S0^T + diag(end) U dS^T + dP^T Q + (E + E^T) K
+//     dg_t = sum over r >= t in the chunk of dG_r, where row r of dG is what its exponent multiplies:
+//         q_r . (dQ's first term)_r + k_r . (dK's first term)_r - k_r . (dK's second term)_r
+//         + row sums - column sums of dP (.) Q K^T + E (.) K K^T,
+//       and dG_last has, besides, the sum of the k . (dK's second term) and gam_last <S0, dS>.
+//
+// Three kinds of kernels: "prepare" (per chunk: T', T, P and the decays; no chunk needs another), "sweeps" (per chain,
+// chunk after chunk: the state and what needs it; the columns of S are independent of each other, so value columns are
+// split over waves and workgroups) and "grad" (per chunk, from the states that two sweeps left).
+#pragma once
+#include "ltn_bf16_tiles.h"
+
+namespace ltn {
+
+constexpr int kChunk = 64;
+
+struct DeltaArgs {
+    const void *q, *k, *v, *d_o;          // [Bt, Hk, N, Dk] twice, [Bt, H, N, Dv] twice
+    void* o;                              // [Bt, H, N, Dv]
+    void *dq, *dk, *dv, *dg, *dbeta;      // as q, k, v; [Bt, H, N] in the tensors' type
+    const float *g, *beta;                // [Bt, H, N]
+    const float* kv_in;                   // [seqs, H, Dk, Dv] or nullptr (zero)
+    float* kv_out;                        // the same, or nullptr
+    const int* cu;                        // packed sequences: their seqs + 1 ends in the one row of N tokens; nullptr: rows are sequences
+    int Hk, H, seqs;                      // seqs = Bt without cu
+    long long N;
+    float scale;
+    // scratch, per (chunk slot, value head): see delta_scratch()
+    char *tq, *tl, *tt, *p, *z, *dy, *s0, *ds;
+    float* vec;
+    int slots;                            // chunk slots of all sequences
+};
+
+// Chunks of a packed sequence are numbered from cu[i] / 64 + i on: no two sequences' overlap, whatever their lengths,
+// and no sum over sequences is needed.
+inline long long delta_slots(long long rows, long long N, bool packed) {
+    return packed ? N / kChunk + rows : rows * ((N + kChunk - 1) / kChunk);
+}
+
+// bytes per (chunk slot, value head) of each scratch array, and all of them for the forward or the backward
+struct DeltaScratch {
+    size_t tile, z, state;                // a 64 x 64 tile, [Dv, 64], [Dv, Dk], in the tensors' type
+    size_t vec;
+};
+inline DeltaScratch delta_scratch(int Dk, int Dv, bool bf16) {
+    const size_t e = bf16 ? 2 : 4;
+    return {kChunk * kChunk * e, Dv * (size_t)kChunk * e, (size_t)Dk * Dv * e, 2 * kChunk * sizeof(float)};
+}
+inline size_t delta_bytes(int Dk, int Dv, bool bf16, bool bwd) {
+    const DeltaScratch s = delta_scratch(Dk, Dv, bf16);
+    // forward: T' (bf16: in two parts), P, decays.  backward: T besides, Z, dY, the states before chunks, their derivatives behind them
+    return (2 + (bf16 ? 1 : 0)) * s.tile + s.vec + (bwd ? s.tile + 2 * s.z + 2 * s.state : 0);
+}
+
+hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
+hipError_t launch_delta_bwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
+hipError_t launch_delta_prepare(const DeltaArgs& a, int Dk, int is_bf16, int is_bwd, hipStream_t stream);
+hipError_t launch_delta_grad(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
+// q, k: [chains of Hk, steps, Dk]; v, o: [chains, steps, Dv]; g, beta: [chains, steps]; kv: [chains, Dk, Dv]
+hipError_t launch_delta_decode(const void* q, const void* k, const void* v, void* o, float* kv, const float* g,
+                               const float* beta, float scale, int Bt, int Hk, int H, int steps, int Dk, int Dv, int is_bf16,
+                               hipStream_t stream);
+
+namespace {
+
+// Where sequence `seq` lies: its first token in its row of N tokens, the row's index among the batch, its length and
+// the slot of its first chunk.  Ends that are out of order or out of the row are drawn into it, so that no access leaves it.
+struct DeltaSeq { long long row, first; int len, slot; };
+__device__ __forceinline__ DeltaSeq delta_seq(const DeltaArgs& a, int seq) {
+    if (!a.cu) return {seq, 0, (int)a.N, seq * (int)((a.N + kChunk - 1) / kChunk)};
+    const int N = (int)a.N, c0 = a.cu[seq], c1 = a.cu[seq + 1];
+    const int first = c0 < 0 ? 0 : (c0 > N ? N : c0), end = c1 < first ? first : (c1 > N ? N : c1);
+    return {0, first, end - first, first / kChunk + seq};
+}
+// The sequence that chunk slot `slot` belongs to, and which of its chunks; false: the slot holds none.
+__device__ __forceinline__ bool delta_find(const DeltaArgs& a, int slot, DeltaSeq& s, int& chunk) {
+    int seq = 0;
+    if (!a.cu) {
+        seq = slot / (int)((a.N + kChunk - 1) / kChunk);
+    } else {
+        int lo = 0, hi = a.seqs - 1;      // the last sequence whose first slot is not behind this one
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (delta_seq(a, mid).slot <= slot) lo = mid;
+            else hi = mid - 1;
+        }
+        seq = lo;
+    }
+    s = delta_seq(a, seq);
+    chunk = slot - s.slot;
+    return chunk >= 0 && (long long)chunk * kChunk < s.len;
+}
+
+// ---- operands of 16 x 16 x 32 products in either type: a lane holds eight consecutive elements of the summed index, from
+// 8 (lane / 16) on.  fp32: eight products of 16 x 16 x 4, each taking one of them from every lane.
+template <class T> struct El;
+template <> struct El<__bf16> {
+    typedef bf16x8 F;
+    static constexpr int PAD = 8;
+};
+struct F32Frag { f32x4 a, b; };
+template <> struct El<float> {
+    typedef F32Frag F;
+    static constexpr int PAD = 4;
+};
+
+__device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) { return mfma16(a, b, c); }
+__device__ __forceinline__ f32x4 mma(const F32Frag& a, const F32Frag& b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.a[j], b.a[j], c, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.b[j], b.b[j], c, 0, 0, 0);
+    return c;
+}
+// eight fp32 values (two tiles' results) as an operand
+template <class T> __device__ __forceinline__ typename El<T>::F frag_of(const f32x4& x, const f32x4& y);
+template <> __device__ __forceinline__ bf16x8 frag_of<__bf16>(const f32x4& x, const f32x4& y) {
+    return __builtin_convertvector(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7), bf16x8);
+}
+template <> __device__ __forceinline__ F32Frag frag_of<float>(const f32x4& x, const f32x4& y) { return {x, y}; }
+__device__ __forceinline__ void values_of(const bf16x8& f, f32x4& x, f32x4& y) {
+    const f32x8 v = __builtin_convertvector(f, f32x8);
+    x = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+    y = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+}
+__device__ __forceinline__ void values_of(const F32Frag& f, f32x4& x, f32x4& y) { x = f.a; y = f.b; }
+// what rounding to the operand's type loses of x, y, as an operand (bf16: 16 bits of the significand together)
+__device__ __forceinline__ bf16x8 rest_of(const bf16x8& f, const f32x4& x, const f32x4& y) {
+    f32x4 a, b;
+    values_of(f, a, b);
+    return frag_of<__bf16>(x - a, y - b);
+}
+
+// A tile's row r holds LD elements.  Eight elements of row `row` from column 32 kb + 8 (lane / 16) on:
+template <class T, int LD> __device__ __forceinline__ typename El<T>::F row_frag(const T* tile, int row, int kb, int lane) {
+    return *(const typename El<T>::F*)(tile + row * LD + kb * 32 + 8 * (lane >> 4));
+}
+// Rows (or columns) of a 16-wide tile whose results, with those of the next tile, are eight consecutive ones in a lane:
+// row m of tile t is 32 (t / 2) + 4 (t % 2) + 8 (m / 4) + m % 4; the lane then holds 32 (t / 2) + 8 (lane / 16) + 4 (t % 2) .. +3.
+__device__ __forceinline__ int paired(int t, int m) { return 32 * (t >> 1) + 4 * (t & 1) + 8 * (m >> 2) + (m & 3); }
+
+// Rows 32 kb + 8 (lane / 16) .. +7 of one column: of column 16 t + lane % 16, or of column paired(t, lane % 16).
+template <int LD, bool PAIRED> __device__ __forceinline__ bf16x8 col_frag(const __bf16* tile, int kb, int t, int lane) {
+    const int s = lane & 15;
+    const int c = PAIRED ? 32 * (t >> 1) + 4 * (t & 1) + 8 * (s & 3) : 16 * t + 4 * (s & 3);
+    const char* p = (const char*)(tile + (kb * 32 + 8 * (lane >> 4) + (s >> 2)) * LD + c);
+    Frag f;
+    f.h[0] = lds_tr16(p);
+    f.h[1] = lds_tr16(p + 4 * LD * sizeof(__bf16));
+    return f.v;
+}
+template <int LD, bool PAIRED> __device__ __forceinline__ F32Frag col_frag(const float* tile, int kb, int t, int lane) {
+    const int c = PAIRED ? paired(t, lane & 15) : 16 * t + (lane & 15);
+    const float* p = tile + (kb * 32 + 8 * (lane >> 4)) * LD + c;
+    F32Frag f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f.a[j] = p[j * LD];
+        f.b[j] = p[(4 + j) * LD];
+    }
+    return f;
+}
+
+// COLS columns of `rows` (at most 64) rows, global -> LDS, by THREADS threads; the tile's other rows become zero.
+template <class T, int LD, int COLS, int THREADS>
+__device__ __forceinline__ void load_tile(T* tile, const T* src, size_t pitch, int rows, int tid) {
+    constexpr int V = 16 / sizeof(T), PER = COLS / V;
+    for (int i = tid; i < kChunk * PER; i += THREADS) {
+        const int r = i / PER, c = i % PER * V;
+        u32x4 x = {0, 0, 0, 0};
+        if (r < rows) x = *(const u32x4*)(src + (size_t)r * pitch + c);
+        *(u32x4*)(tile + r * LD + c) = x;
+    }
+}
+
+}  // namespace
+}  // namespace ltn

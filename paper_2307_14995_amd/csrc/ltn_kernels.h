@@ -189,6 +189,15 @@ hipError_t launch_prologue(const void* x, const float* theta, const void* dy, vo
 hipError_t launch_gate(const void* x, const void* u, const void* dy, void* o0, void* o1, float eps,
                        long long rows, int D, int is_bf16, int is_bwd, hipStream_t stream);
 
+// The norms around a block (see ltn_block_norm.hip) on `rows` rows of C features; `gates` rows of gates, each for rows / gates
+// consecutive rows.  is_bwd = 0: o0 = x_out, o1 = h.  is_bwd = 1: o0 = dx, o1 = dy; part: block_norm_part_floats() floats.
+long long block_norm_strip(long long rows, int C, bool bwd);
+size_t block_norm_part_floats(long long rows, int C);
+hipError_t launch_block_norm(const void* x, const void* y, const void* gate, const float* w_after, const float* w_before,
+                             const void* d_x_out, const void* d_h, void* o0, void* o1, void* d_gate, float* dwa, float* dwb,
+                             float* part, float scale, float eps, int after, long long rows, long long gates, int C,
+                             int is_bf16, int is_bwd, hipStream_t stream);
+
 // Streaming-read probe (see ltn_probe.hip): wgs workgroups each read their own per_wg bytes
 // (a multiple of 64 KB) of `buf` `iters` times, to LDS directly or to registers.
 hipError_t launch_probe_stream(const void* buf, size_t per_wg, int wgs, int iters, int to_registers, unsigned* sink,
