@@ -64,7 +64,7 @@ struct DeltaScratch {
 };
 inline DeltaScratch delta_scratch(int Dk, int Dv, bool bf16) {
     const size_t e = bf16 ? 2 : 4;
-    return {kChunk * kChunk * e, Dv * (size_t)kChunk * e, (size_t)Dk * Dv * e, 2 * kChunk * sizeof(float)};
+    return {kChunk * kChunk * e, Dv * (size_t)kChunk * e, (size_t)Dk * Dv * e, 3 * kChunk * sizeof(float)};
 }
 inline size_t delta_bytes(int Dk, int Dv, bool bf16, bool bwd) {
     const DeltaScratch s = delta_scratch(Dk, Dv, bf16);
@@ -151,27 +151,116 @@ __device__ __forceinline__ bf16x8 rest_of(const bf16x8& f, const f32x4& x, const
     return frag_of<__bf16>(x - a, y - b);
 }
 
-// A tile's row r holds LD elements.  Eight elements of row `row` from column 32 kb + 8 (lane / 16) on:
-template <class T, int LD> __device__ __forceinline__ typename El<T>::F row_frag(const T* tile, int row, int kb, int lane) {
-    return *(const typename El<T>::F*)(tile + row * LD + kb * 32 + 8 * (lane >> 4));
+// ---- LDS tiles of 64 rows (tokens, or columns of a state) and COLS columns.  bf16: as Swz has it (16-byte chunks swizzled
+// with the row, no padding), filled by direct loads.  fp32: rows padded by 16 bytes, filled through registers.
+template <class T, int COLS> struct Tile;
+template <int COLS> struct Tile<__bf16, COLS> {
+    static constexpr int RB = Swz<COLS>::RB, BYTES = Swz<COLS>::BYTES;
+    static __device__ __forceinline__ int chunk(int r, int c) { return Swz<COLS>::off(r, c); }    // of 16 bytes
+    static __device__ __forceinline__ int at(int r, int c) { return chunk(r, c >> 3) + (c & 7) * 2; }
+};
+template <int COLS> struct Tile<float, COLS> {
+    static constexpr int RB = COLS * 4 + 16, BYTES = kChunk * RB;
+    static __device__ __forceinline__ int chunk(int r, int c) { return r * RB + c * 16; }
+    static __device__ __forceinline__ int at(int r, int c) { return r * RB + c * 4; }
+};
+
+// Eight elements of row `row` from column 32 kb + 8 (lane / 16) on:
+template <class T, int COLS> __device__ __forceinline__ typename El<T>::F row_frag(const char* tile, int row, int kb, int lane) {
+    if constexpr (sizeof(T) == 2) return *(const bf16x8*)(tile + Tile<T, COLS>::chunk(row, 4 * kb + (lane >> 4)));
+    else return *(const F32Frag*)(tile + Tile<T, COLS>::chunk(row, 8 * kb + 2 * (lane >> 4)));
 }
 // Rows (or columns) of a 16-wide tile whose results, with those of the next tile, are eight consecutive ones in a lane:
 // row m of tile t is 32 (t / 2) + 4 (t % 2) + 8 (m / 4) + m % 4; the lane then holds 32 (t / 2) + 8 (lane / 16) + 4 (t % 2) .. +3.
 __device__ __forceinline__ int paired(int t, int m) { return 32 * (t >> 1) + 4 * (t & 1) + 8 * (m >> 2) + (m & 3); }
 
 // Rows 32 kb + 8 (lane / 16) .. +7 of one column: of column 16 t + lane % 16, or of column paired(t, lane % 16).
-template <int LD, bool PAIRED> __device__ __forceinline__ bf16x8 col_frag(const __bf16* tile, int kb, int t, int lane) {
+template <class T, int COLS, bool PAIRED> __device__ __forceinline__ typename El<T>::F col_frag(const char* tile, int kb, int t, int lane) {
+    const int row = kb * 32 + 8 * (lane >> 4), s = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+        const int c = PAIRED ? 32 * (t >> 1) + 4 * (t & 1) + 8 * (s & 3) : 16 * t + 4 * (s & 3);
+        Frag f;
+        f.h[0] = lds_tr16(tile + Tile<T, COLS>::at(row + (s >> 2), c));
+        f.h[1] = lds_tr16(tile + Tile<T, COLS>::at(row + 4 + (s >> 2), c));
+        return f.v;
+    } else {
+        const float* p = (const float*)(tile + Tile<T, COLS>::at(row, PAIRED ? paired(t, s) : 16 * t + s));
+        constexpr int LD = Tile<T, COLS>::RB / 4;
+        F32Frag f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f.a[j] = p[j * LD];
+            f.b[j] = p[(4 + j) * LD];
+        }
+        return f;
+    }
+}
+// Rows 32 (rt / 2) + 8 (lane / 16) + 4 (rt % 2) .. +3 of column c0 + lane % 16, as fp32
+template <class T, int COLS> __device__ __forceinline__ f32x4 col_values(const char* tile, int rt, int c0, int lane) {
+    const int row = 32 * (rt >> 1) + 8 * (lane >> 4) + 4 * (rt & 1), s = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+        Frag f;
+        f.h[0] = lds_tr16(tile + Tile<T, COLS>::at(row + (s >> 2), c0 + 4 * (s & 3)));
+        return __builtin_convertvector(f.b[0], f32x4);
+    } else {
+        const float* p = (const float*)(tile + Tile<T, COLS>::at(row, c0 + s));
+        constexpr int LD = Tile<T, COLS>::RB / 4;
+        return f32x4{p[0], p[LD], p[2 * LD], p[3 * LD]};
+    }
+}
+
+// A tile from global memory, rows `pitch` bytes apart, by W waves; rows from `valid` on become zero.  bf16: fetch() issues
+// direct loads to LDS and the data is there once they have been waited for.  fp32: fetch() loads registers, put() stores them.
+template <class T, int COLS, int W, int ROWS = kChunk> struct TileFetch;
+template <int COLS, int W, int ROWS> struct TileFetch<__bf16, COLS, W, ROWS> {
+    typedef Swz<COLS> S;
+    static constexpr int NV = S::CPR / 4, NI = S::NI * ROWS / kChunk, PER = NI / W;      // loads of a tile and of a wave
+    static_assert(NI % W == 0 && NV >= 1, "every wave issues the same number of loads");
+    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, char* tile, int w, int lane) {
+        const unsigned lds = lds_address(tile);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = w + W * i, slot = 64 * j + lane, r = slot / S::CPR, c = (slot % S::CPR) ^ S::key(r);
+            const char* g = src + (size_t)r * pitch + c * 16;
+            dma16(lds + 1024u * (unsigned)j, r < valid ? g : (const char*)kZeros);
+        }
+    }
+    __device__ __forceinline__ void put(char*, int, int) const {}
+};
+template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
+    static constexpr int CPR = COLS / 4, PER = ROWS * CPR / (64 * W);
+    u32x4 v[PER];
+    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, char*, int w, int lane) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = 64 * (w + W * i) + lane, r = j / CPR;
+            v[i] = u32x4{0, 0, 0, 0};
+            if (r < valid) v[i] = *(const u32x4*)(src + (size_t)r * pitch + j % CPR * 16);
+        }
+    }
+    __device__ __forceinline__ void put(char* tile, int w, int lane) const {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int j = 64 * (w + W * i) + lane;
+            *(u32x4*)(tile + Tile<float, COLS>::chunk(j / CPR, j % CPR)) = v[i];
+        }
+    }
+};
+
+// ---- plain padded tiles of LD elements a row (the kernels that are not sweeps)
+template <class T, int LD> __device__ __forceinline__ typename El<T>::F row_frag_p(const T* tile, int row, int kb, int lane) {
+    return *(const typename El<T>::F*)(tile + row * LD + kb * 32 + 8 * (lane >> 4));
+}
+template <int LD> __device__ __forceinline__ bf16x8 col_frag_p(const __bf16* tile, int kb, int t, int lane) {
     const int s = lane & 15;
-    const int c = PAIRED ? 32 * (t >> 1) + 4 * (t & 1) + 8 * (s & 3) : 16 * t + 4 * (s & 3);
-    const char* p = (const char*)(tile + (kb * 32 + 8 * (lane >> 4) + (s >> 2)) * LD + c);
+    const char* p = (const char*)(tile + (kb * 32 + 8 * (lane >> 4) + (s >> 2)) * LD + 16 * t + 4 * (s & 3));
     Frag f;
     f.h[0] = lds_tr16(p);
     f.h[1] = lds_tr16(p + 4 * LD * sizeof(__bf16));
     return f.v;
 }
-template <int LD, bool PAIRED> __device__ __forceinline__ F32Frag col_frag(const float* tile, int kb, int t, int lane) {
-    const int c = PAIRED ? paired(t, lane & 15) : 16 * t + (lane & 15);
-    const float* p = tile + (kb * 32 + 8 * (lane >> 4)) * LD + c;
+template <int LD> __device__ __forceinline__ F32Frag col_frag_p(const float* tile, int kb, int t, int lane) {
+    const float* p = tile + (kb * 32 + 8 * (lane >> 4)) * LD + 16 * t + (lane & 15);
     F32Frag f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

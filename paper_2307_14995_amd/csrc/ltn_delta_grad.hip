@@ -85,8 +85,8 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             }
             l.Gs[lane] = x;
             l.beta[lane] = lane < rows ? a.beta[val_row + lane] : 0.f;
-            l.gam[lane] = a.vec[at * 2 * kChunk + lane];
-            l.end[lane] = a.vec[at * 2 * kChunk + kChunk + lane];
+            l.gam[lane] = a.vec[at * 3 * kChunk + lane];
+            l.end[lane] = a.vec[at * 3 * kChunk + kChunk + lane];
         }
         f32x4 dP[4], E[4], qs[NT], ks[NT], ke[NT];
 #pragma unroll
@@ -108,9 +108,9 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             }
 #pragma unroll
             for (int kb = 0; kb < VS / 32; ++kb) {
-                const F g = row_frag<T, LV>(l.slab.G, 16 * w + m, kb, lane);
-                const F y = col_frag<LT, false>(l.slab.Y, kb, w, lane);
-                const F z = col_frag<LT, false>(l.slab.Z, kb, w, lane);
+                const F g = row_frag_p<T, LV>(l.slab.G, 16 * w + m, kb, lane);
+                const F y = col_frag_p<LT>(l.slab.Y, kb, w, lane);
+                const F z = col_frag_p<LT>(l.slab.Z, kb, w, lane);
                 db += dot8<T>(y, z);
                 if (16 * w + m < rows) {
                     f32x4 y0, y1;
@@ -121,13 +121,13 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
 #pragma unroll
                 for (int ct = 0; ct < 4; ++ct) {
                     if (ct > w) continue;
-                    const F b = col_frag<LT, false>(l.slab.Z, kb, ct, lane);
+                    const F b = col_frag_p<LT>(l.slab.Z, kb, ct, lane);
                     dP[ct] = mma(g, b, dP[ct]);
                     E[ct] = mma(y, b, E[ct]);
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const F b = col_frag<LD, false>(l.slab.S, kb, t, lane), d = col_frag<LD, false>(l.slab.D, kb, t, lane);
+                    const F b = col_frag_p<LD>(l.slab.S, kb, t, lane), d = col_frag_p<LD>(l.slab.D, kb, t, lane);
                     qs[t] = mma(g, b, qs[t]);
                     ks[t] = mma(y, b, ks[t]);
                     ke[t] = mma(z, d, ke[t]);
@@ -152,9 +152,9 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             if (ct <= w) {
 #pragma unroll
                 for (int kb = 0; kb < DK / 32; ++kb) {
-                    const F b = row_frag<T, LD>(l.K, c, kb, lane);
-                    kk = mma(row_frag<T, LD>(l.K, 16 * w + m, kb, lane), b, kk);
-                    qk = mma(row_frag<T, LD>(l.Q, 16 * w + m, kb, lane), b, qk);
+                    const F b = row_frag_p<T, LD>(l.K, c, kb, lane);
+                    kk = mma(row_frag_p<T, LD>(l.K, 16 * w + m, kb, lane), b, kk);
+                    qk = mma(row_frag_p<T, LD>(l.Q, 16 * w + m, kb, lane), b, qk);
                 }
             }
             const double gc = l.Gs[c];
@@ -213,14 +213,14 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             f32x4 x = dq[t] + qs[t], y = dk[t] + ks[t] + ke[t];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const F kf = col_frag<LD, false>(l.K, kb, t, lane);
+                const F kf = col_frag_p<LD>(l.K, kb, t, lane);
                 if (kb <= w / 2) {
-                    x = mma(row_frag<T, LT>(l.chunk.dP, 16 * w + m, kb, lane), kf, x);
-                    y = mma(row_frag<T, LT>(l.chunk.E, 16 * w + m, kb, lane), kf, y);
+                    x = mma(row_frag_p<T, LT>(l.chunk.dP, 16 * w + m, kb, lane), kf, x);
+                    y = mma(row_frag_p<T, LT>(l.chunk.E, 16 * w + m, kb, lane), kf, y);
                 }
                 if (kb >= w / 2) {
-                    y = mma(col_frag<LT, false>(l.chunk.dP, kb, w, lane), col_frag<LD, false>(l.Q, kb, t, lane), y);
-                    y = mma(col_frag<LT, false>(l.chunk.E, kb, w, lane), kf, y);
+                    y = mma(col_frag_p<LT>(l.chunk.dP, kb, w, lane), col_frag_p<LD>(l.Q, kb, t, lane), y);
+                    y = mma(col_frag_p<LT>(l.chunk.E, kb, w, lane), kf, y);
                 }
             }
             dq[t] = x;

@@ -73,9 +73,10 @@ void delta_prepare_kernel(DeltaArgs a) {
         G[lane] = x;
         B[lane] = lane < rows ? a.beta[gate_row + lane] : 0.f;
         const double last = __shfl(x, 63, 64);
-        float* const vec = a.vec + at * 2 * kChunk;
+        float* const vec = a.vec + at * 3 * kChunk;
         vec[lane] = expf((float)x);
         vec[kChunk + lane] = expf((float)(last - x));
+        vec[2 * kChunk + lane] = B[lane];
     }
     for (int i = tid; i < (BWD ? 2 : 1) * kChunk * LA; i += kThreads) inv[i] = 0.f;
     __syncthreads();
@@ -88,9 +89,9 @@ void delta_prepare_kernel(DeltaArgs a) {
         if (ct > w) continue;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
-            const auto b = row_frag<T, LD>(K, 16 * ct + m, kb, lane);
-            kk[ct] = mma(row_frag<T, LD>(K, 16 * w + m, kb, lane), b, kk[ct]);
-            qk[ct] = mma(row_frag<T, LD>(Q, 16 * w + m, kb, lane), b, qk[ct]);
+            const auto b = row_frag_p<T, LD>(K, 16 * ct + m, kb, lane);
+            kk[ct] = mma(row_frag_p<T, LD>(K, 16 * w + m, kb, lane), b, kk[ct]);
+            qk[ct] = mma(row_frag_p<T, LD>(Q, 16 * w + m, kb, lane), b, qk[ct]);
         }
     }
     __syncthreads();

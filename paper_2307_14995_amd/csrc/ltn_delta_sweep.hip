@@ -12,41 +12,78 @@
 namespace ltn {
 namespace {
 
-// v - gam (K S) etc. for the four tokens that a lane holds of row tile rt: 32 (rt / 2) + 8 (lane / 16) + 4 (rt % 2) .. +3
+// first of the four tokens (or features) that a lane holds of row tile rt
 __device__ __forceinline__ int token_of(int rt, int grp) { return 32 * (rt >> 1) + 8 * grp + 4 * (rt & 1); }
 
-// Columns of a wave in a [token][column] LDS tile for the lane's four tokens of row tile rt
-template <int LD> __device__ __forceinline__ f32x4 col_values(const __bf16* tile, int rt, int c0, int lane) {
-    const int s = lane & 15;
-    Frag f;
-    f.h[0] = lds_tr16((const char*)(tile + (token_of(rt, lane >> 4) + (s >> 2)) * LD + c0 + 4 * (s & 3)));
-    return __builtin_convertvector(f.b[0], f32x4);
-}
-template <int LD> __device__ __forceinline__ f32x4 col_values(const float* tile, int rt, int c0, int lane) {
-    const float* p = tile + token_of(rt, lane >> 4) * LD + c0 + (lane & 15);
-    return f32x4{p[0], p[LD], p[2 * LD], p[3 * LD]};
-}
-
 template <class T> __device__ __forceinline__ void store_frag(T* p, const typename El<T>::F& f) { *(typename El<T>::F*)p = f; }
+// four fp32 values as four consecutive elements
+__device__ __forceinline__ void store4(__bf16* p, const f32x4& x) { *(bf16x4*)p = to_bf16(x); }
+__device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
+
+// One chunk's tiles in LDS.  FWD: K, T', its second part (bf16), V and, where O is wanted, Q and P.  Backward: K, Q, T, P, dO.
+template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
+    static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
+                         T2 = VEC + 1024, Q = T2 + (FWD && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
+                         P = Q + (FULL ? Tile<T, DK>::BYTES : 0), BYTES = P + (FULL ? Tile<T, kChunk>::BYTES : 0);
+    static constexpr int BUFS = 2 * BYTES <= 160 * 1024 ? 2 : 1;
+};
+
+// The fetches of a chunk's tiles by W waves.
+template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFetch {
+    typedef SweepLds<T, DK, COLS, FULL, FWD> L;
+    static constexpr bool BF = sizeof(T) == 2;
+    static constexpr size_t kTile = (size_t)kChunk * kChunk * sizeof(T);
+    TileFetch<T, DK, W> k, q;
+    TileFetch<T, kChunk, W> t1, t2, p;
+    TileFetch<T, COLS, W> v;
+    u32x4 vec;
+    // at: the chunk's scratch; key_row, val_row: its first token's rows
+    __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t at, size_t key_row, size_t val_row, int rows, int Dv, int col0,
+                                          char* lds, int w, int lane) {
+        k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::K, w, lane);
+        t1.fetch((FWD ? a.tq : a.tt) + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T1, w, lane);
+        v.fetch((const char*)(FWD ? a.v : a.d_o) + (val_row * Dv + col0) * sizeof(T), Dv * sizeof(T), rows, lds + L::V, w, lane);
+        if constexpr (FWD && BF) t2.fetch(a.tl + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T2, w, lane);
+        if constexpr (FULL) {
+            q.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::Q, w, lane);
+            p.fetch(a.p + at * kTile, kChunk * sizeof(T), kChunk, lds + L::P, w, lane);
+        }
+        if (w == 0) {                      // 768 bytes of decays and beta (the last quarter of the kilobyte is not read)
+            const char* src = (const char*)(a.vec + at * 3 * kChunk) + (lane < 48 ? lane * 16 : 0);
+            if constexpr (BF) dma16(lds_address(lds + L::VEC), src);
+            else vec = *(const u32x4*)src;
+        }
+    }
+    __device__ __forceinline__ void put(char* lds, int w, int lane) const {
+        if constexpr (!BF) {
+            k.put(lds + L::K, w, lane);
+            t1.put(lds + L::T1, w, lane);
+            v.put(lds + L::V, w, lane);
+            if constexpr (FULL) {
+                q.put(lds + L::Q, w, lane);
+                p.put(lds + L::P, w, lane);
+            }
+            if (w == 0) *(u32x4*)(lds + L::VEC + lane * 16) = vec;
+        }
+    }
+};
 
 // Forward.  SAVE: Z and the states before chunks are written, for the gradients, and O is not.
 template <class T, int DK, int CT, int W, bool SAVE>
 __global__ __launch_bounds__(64 * W)
 void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int LD = DK + El<T>::PAD, LT = kChunk + El<T>::PAD, COLS = 16 * CT * W, LV = COLS + El<T>::PAD;
-    constexpr int NT = DK / 16, TH = 64 * W;
+    constexpr int COLS = 16 * CT * W, NT = DK / 16;
     typedef typename El<T>::F F;
-    __shared__ __attribute__((aligned(16))) T K[kChunk * LD], Q[SAVE ? 8 : kChunk * LD], Tq[kChunk * LT], Tl[BF ? kChunk * LT : 8],
-        P[SAVE ? 8 : kChunk * LT], V[kChunk * LV];
-    __shared__ __attribute__((aligned(16))) float vec[3 * kChunk];       // gam, end, beta
+    typedef SweepLds<T, DK, COLS, !SAVE, true> L;
+    constexpr bool TWO = BF && L::BUFS == 2;
+    __shared__ __attribute__((aligned(1024))) char lds[(TWO ? 2 : 1) * L::BYTES];
 
     int chain, split;
-    const int chains = a.seqs * a.H;
-    map_workgroup(blockIdx.x, per_chain, chains, chain, split);
+    map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
     const int wg0 = split * COLS, c0 = 16 * CT * w;                      // the workgroup's and the wave's first column
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
@@ -64,20 +101,30 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             }
     }
     const int chunks = (s.len + kChunk - 1) / kChunk;
+    SweepFetch<T, DK, COLS, W, !SAVE, true> next;
+    auto fetch = [&](int chunk) {
+        const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
+        next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
+                   lds + (TWO ? (chunk & 1) * L::BYTES : 0), w, lane);
+    };
+    if (chunks) fetch(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        __syncthreads();
-        load_tile<T, LD, DK, TH>(K, (const T*)a.k + (key_row + t0) * DK, DK, rows, tid);
-        if constexpr (!SAVE) load_tile<T, LD, DK, TH>(Q, (const T*)a.q + (key_row + t0) * DK, DK, rows, tid);
-        load_tile<T, LV, COLS, TH>(V, (const T*)a.v + (val_row + t0) * Dv + wg0, Dv, rows, tid);
-        constexpr size_t kTile = (size_t)kChunk * kChunk * sizeof(T);
-        load_tile<T, LT, kChunk, TH>(Tq, (const T*)(a.tq + at * kTile), kChunk, kChunk, tid);
-        if constexpr (BF) load_tile<T, LT, kChunk, TH>(Tl, (const T*)(a.tl + at * kTile), kChunk, kChunk, tid);
-        if constexpr (!SAVE) load_tile<T, LT, kChunk, TH>(P, (const T*)(a.p + at * kTile), kChunk, kChunk, tid);
-        for (int i = tid; i < 3 * kChunk; i += TH)
-            vec[i] = i < 2 * kChunk ? a.vec[at * 2 * kChunk + i] : (i - 2 * kChunk < rows ? a.beta[val_row + t0 + i - 2 * kChunk] : 0.f);
-        __syncthreads();
+        const char* const cur = lds + (TWO ? (chunk & 1) * L::BYTES : 0);
+        if constexpr (TWO) {
+            wait_dma<0>();
+            __syncthreads();               // this chunk's tiles are there, the last one's are read
+            if (chunk + 1 < chunks) fetch(chunk + 1);
+        } else {
+            if (BF) wait_dma<0>();
+            next.put(lds, w, lane);
+            __syncthreads();
+            if (!BF && chunk + 1 < chunks) fetch(chunk + 1);
+        }
+        const char *const K = cur + L::K, *const Tq = cur + L::T1, *const Tl = cur + L::T2, *const V = cur + L::V,
+                   *const Q = cur + L::Q, *const P = cur + L::P;
+        const float* const vec = (const float*)(cur + L::VEC);           // gam, end, beta
         const float whole = vec[kChunk - 1];
 
 #pragma unroll
@@ -88,43 +135,44 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             for (int p = 0; p < NT / 2; ++p) {
                 Sh[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
                 if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p][c], S[2 * p + 1][c]);
-                if constexpr (SAVE) {
-                    T* const out = (T*)a.s0 + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp;
-                    store_frag<T>(out, Sh[p]);
-                }
+                if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sh[p]);
             }
             f32x4 Z[4], O[4];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
-                O[rt] = x;
-                const int row = paired(rt, m);
+            for (int rt = 0; rt < 4; ++rt) Z[rt] = O[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int p = 0; p < NT / 2; ++p) {
-                    const F kf = row_frag<T, LD>(K, row, p, lane);
-                    x = mma(kf, Sh[p], x);
-                    if constexpr (BF) x = mma(kf, Sl[p], x);
-                    if constexpr (!SAVE) O[rt] = mma(row_frag<T, LD>(Q, row, p, lane), Sh[p], O[rt]);
+            for (int p = 0; p < NT / 2; ++p)
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) {
+                    const F kf = row_frag<T, DK>(K, paired(rt, m), p, lane);
+                    Z[rt] = mma(kf, Sh[p], Z[rt]);
+                    if constexpr (BF) Z[rt] = mma(kf, Sl[p], Z[rt]);
                 }
-                const f32x4 gam = *(const f32x4*)(vec + token_of(rt, grp));
-                Z[rt] = col_values<LV>(V, rt, col, lane) - gam * x;
-                if constexpr (!SAVE) O[rt] *= gam * a.scale;
-            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt)
+                Z[rt] = col_values<T, COLS>(V, rt, col, lane) - *(const f32x4*)(vec + token_of(rt, grp)) * Z[rt];
             F Xh[2], Xl[BF ? 2 : 1];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 Xh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
                 if constexpr (BF) Xl[b] = rest_of(Xh[b], Z[2 * b], Z[2 * b + 1]);
             }
+            // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory
+            if constexpr (!SAVE) {
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt)
+                for (int p = 0; p < NT / 2; ++p)
 #pragma unroll
-                for (int b = 0; b <= rt / 2; ++b) {
-                    const F tf = row_frag<T, LT>(Tq, paired(rt, m), b, lane);
+                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], row_frag<T, DK>(Q, 16 * rt + m, p, lane), O[rt]);
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int rt = 2 * b; rt < 4; ++rt) {
+                    const F tf = row_frag<T, kChunk>(Tq, paired(rt, m), b, lane);
                     Z[rt] = mma(tf, Xh[b], Z[rt]);
                     if constexpr (BF) {
                         Z[rt] = mma(tf, Xl[b], Z[rt]);
-                        Z[rt] = mma(row_frag<T, LT>(Tl, paired(rt, m), b, lane), Xh[b], Z[rt]);
+                        Z[rt] = mma(row_frag<T, kChunk>(Tl, paired(rt, m), b, lane), Xh[b], Z[rt]);
                     }
                 }
             F Uh[2], Ul[BF ? 2 : 1];
@@ -139,9 +187,11 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt)
+                for (int rt = 0; rt < 4; ++rt) {
+                    O[rt] *= vec[16 * rt + m] * a.scale;
 #pragma unroll
-                    for (int b = 0; b <= rt / 2; ++b) O[rt] = mma(row_frag<T, LT>(P, paired(rt, m), b, lane), Uh[b], O[rt]);
+                    for (int b = 0; b <= rt / 2; ++b) O[rt] = mma(Uh[b], row_frag<T, kChunk>(P, 16 * rt + m, b, lane), O[rt]);
+                }
             }
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) Z[rt] *= *(const f32x4*)(vec + kChunk + token_of(rt, grp));
@@ -151,31 +201,24 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 if constexpr (BF) Ul[b] = rest_of(Uh[b], Z[2 * b], Z[2 * b + 1]);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                S[t][c] *= whole;
+            for (int t = 0; t < NT; ++t) S[t][c] *= whole;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const F kf = col_frag<LD, true>(K, b, t, lane);
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const F kf = col_frag<T, DK, true>(K, b, t, lane);
                     S[t][c] = mma(kf, Uh[b], S[t][c]);
                     if constexpr (BF) S[t][c] = mma(kf, Ul[b], S[t][c]);
                 }
-            }
             if constexpr (!SAVE) {
-                // the wave's columns of V have been read: O takes their place and is read back a token a row
 #pragma unroll
                 for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) V[(token_of(rt, grp) + i) * LV + col + m] = (T)O[rt][i];
+                    if (16 * rt + m < rows) store4((T*)a.o + (val_row + t0 + 16 * rt + m) * Dv + wg0 + col + 4 * grp, O[rt]);
             }
         }
-        if constexpr (!SAVE) {
-            constexpr int E = 16 / sizeof(T), PER = 16 * CT / E;         // pieces of 16 bytes of a token's columns of this wave
-            asm volatile("" : : : "memory");                             // (a wave's LDS accesses stay in order; so does the compiler)
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int r = (i * 64 + lane) / PER, c = c0 + (i * 64 + lane) % PER * E;
-                if (r < rows) *(u32x4*)((T*)a.o + (val_row + t0 + r) * Dv + wg0 + c) = *(const u32x4*)(V + r * LV + c);
-            }
+        if constexpr (!TWO) {
+            __syncthreads();
+            if (BF && chunk + 1 < chunks) fetch(chunk + 1);
         }
     }
     if (!SAVE && a.kv_out) {
@@ -193,18 +236,18 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 template <class T, int DK, int CT, int W>
 __global__ __launch_bounds__(64 * W)
 void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
-    constexpr int LD = DK + El<T>::PAD, LT = kChunk + El<T>::PAD, COLS = 16 * CT * W, LV = COLS + El<T>::PAD;
-    constexpr int NT = DK / 16, TH = 64 * W;
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int COLS = 16 * CT * W, NT = DK / 16;
     typedef typename El<T>::F F;
-    __shared__ __attribute__((aligned(16))) T K[kChunk * LD], Q[kChunk * LD], Tt[kChunk * LT], P[kChunk * LT], G[kChunk * LV];
-    __shared__ __attribute__((aligned(16))) float vec[3 * kChunk];
+    typedef SweepLds<T, DK, COLS, true, false> L;
+    constexpr bool TWO = BF && L::BUFS == 2;
+    __shared__ __attribute__((aligned(1024))) char lds[(TWO ? 2 : 1) * L::BYTES];
 
     int chain, split;
-    const int chains = a.seqs * a.H;
-    map_workgroup(blockIdx.x, per_chain, chains, chain, split);
+    map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
     const int wg0 = split * COLS, c0 = 16 * CT * w;
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
@@ -215,19 +258,28 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) S[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int chunks = (s.len + kChunk - 1) / kChunk;
-    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+    SweepFetch<T, DK, COLS, W, true, false> next;
+    auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
+        next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
+                   lds + (TWO ? (chunk & 1) * L::BYTES : 0), w, lane);
+    };
+    if (chunks) fetch(chunks - 1);
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        __syncthreads();
-        load_tile<T, LD, DK, TH>(K, (const T*)a.k + (key_row + t0) * DK, DK, rows, tid);
-        load_tile<T, LD, DK, TH>(Q, (const T*)a.q + (key_row + t0) * DK, DK, rows, tid);
-        load_tile<T, LV, COLS, TH>(G, (const T*)a.d_o + (val_row + t0) * Dv + wg0, Dv, rows, tid);
-        constexpr size_t kTile = (size_t)kChunk * kChunk * sizeof(T);
-        load_tile<T, LT, kChunk, TH>(Tt, (const T*)(a.tt + at * kTile), kChunk, kChunk, tid);
-        load_tile<T, LT, kChunk, TH>(P, (const T*)(a.p + at * kTile), kChunk, kChunk, tid);
-        for (int i = tid; i < 3 * kChunk; i += TH)
-            vec[i] = i < 2 * kChunk ? a.vec[at * 2 * kChunk + i] : (i - 2 * kChunk < rows ? a.beta[val_row + t0 + i - 2 * kChunk] : 0.f);
-        __syncthreads();
+        const char* const cur = lds + (TWO ? (chunk & 1) * L::BYTES : 0);
+        if constexpr (TWO) {
+            wait_dma<0>();
+            __syncthreads();
+            if (chunk) fetch(chunk - 1);
+        } else {
+            if (BF) wait_dma<0>();
+            next.put(lds, w, lane);
+            __syncthreads();
+            if (!BF && chunk) fetch(chunk - 1);
+        }
+        const char *const K = cur + L::K, *const Tt = cur + L::T1, *const G = cur + L::V, *const Q = cur + L::Q, *const P = cur + L::P;
+        const float* const vec = (const float*)(cur + L::VEC);
         const float whole = vec[kChunk - 1];
 
 #pragma unroll
@@ -241,16 +293,19 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             }
             F gf[2];                       // dO
 #pragma unroll
-            for (int b = 0; b < 2; ++b) gf[b] = col_frag<LV, false>(G + col, b, 0, lane);
+            for (int b = 0; b < 2; ++b) gf[b] = col_frag<T, COLS, false>(G, b, col / 16, lane);
             f32x4 Y[4];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                Y[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int rt = 0; rt < 4; ++rt) Y[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int p = 0; p < NT / 2; ++p) Y[rt] = mma(row_frag<T, LD>(K, paired(rt, m), p, lane), Sf[p], Y[rt]);
+            for (int p = 0; p < NT / 2; ++p)
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(row_frag<T, DK>(K, paired(rt, m), p, lane), Sf[p], Y[rt]);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
                 Y[rt] *= *(const f32x4*)(vec + kChunk + token_of(rt, grp));
 #pragma unroll
-                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<LT, true>(P, b, rt, lane), gf[b], Y[rt]);
+                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<T, kChunk, true>(P, b, rt, lane), gf[b], Y[rt]);
             }
             F uf[2];
 #pragma unroll
@@ -258,7 +313,7 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<LT, true>(Tt, b, rt, lane), uf[b], Y[rt]);
+                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<T, kChunk, true>(Tt, b, rt, lane), uf[b], Y[rt]);
             F xf[2], of[2];                // -gam dV, scale gam dO
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -271,14 +326,18 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 of[b] = frag_of<T>(a.scale * g0 * o0, a.scale * g1 * o1);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                S[t][c] *= whole;
+            for (int t = 0; t < NT; ++t) S[t][c] *= whole;
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    S[t][c] = mma(col_frag<LD, true>(K, b, t, lane), xf[b], S[t][c]);
-                    S[t][c] = mma(col_frag<LD, true>(Q, b, t, lane), of[b], S[t][c]);
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    S[t][c] = mma(col_frag<T, DK, true>(Q, b, t, lane), of[b], S[t][c]);
+                    S[t][c] = mma(col_frag<T, DK, true>(K, b, t, lane), xf[b], S[t][c]);
                 }
-            }
+        }
+        if constexpr (!TWO) {
+            __syncthreads();
+            if (BF && chunk) fetch(chunk - 1);
         }
     }
 }
