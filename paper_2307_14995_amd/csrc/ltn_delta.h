@@ -19,10 +19,10 @@
 //     dP = scale R (.) dO U^T      E = -R (.) diag(beta) dY U^T below the diagonal
 //     dQ = scale diag(gam) dO S0^T + dP K
 //     dK = -diag(gam) dV S0^T + diag(end) U dS^T + dP^T Q + (E + E^T) K
-//     dg_t = sum over r >= t in the chunk of dG_r, where row r of dG is what its exponent multiplies:
-//         q_r . (dQ's first term)_r + k_r . (dK's first term)_r - k_r . (dK's second term)_r
-//         + row sums - column sums of dP (.) Q K^T + E (.) K K^T,
-//       and dG_last has, besides, the sum of the k . (dK's second term) and gam_last <S0, dS>.
+//     dg_t = sum over r >= t in the chunk of dG_r,
+//     dG_r = q_r . (dQ's first term)_r + k_r . (dK's first term)_r - k_r . (dK's second term)_r
+//            + row r's sums - column r's sums of dP (.) Q K^T and E (.) K K^T,
+//     and dG_last has, besides, the sum of the k . (dK's second term) and gam_last <S0, dS>.
 //
 // Three kinds of kernels: "prepare" (per chunk: T', T, P and the decays; no chunk needs another), "sweeps" (per chain,
 // chunk after chunk: the state and what needs it; the columns of S are independent of each other, so value columns are
@@ -33,6 +33,7 @@
 namespace ltn {
 
 constexpr int kChunk = 64;
+constexpr int kVec = 5 * kChunk;          // per chunk: gam, end, beta and G in two parts (G = hi + lo)
 
 struct DeltaArgs {
     const void *q, *k, *v, *d_o;          // [Bt, Hk, N, Dk] twice, [Bt, H, N, Dv] twice
@@ -64,7 +65,7 @@ struct DeltaScratch {
 };
 inline DeltaScratch delta_scratch(int Dk, int Dv, bool bf16) {
     const size_t e = bf16 ? 2 : 4;
-    return {kChunk * kChunk * e, Dv * (size_t)kChunk * e, (size_t)Dk * Dv * e, 3 * kChunk * sizeof(float)};
+    return {kChunk * kChunk * e, Dv * (size_t)kChunk * e, (size_t)Dk * Dv * e, kVec * sizeof(float)};
 }
 inline size_t delta_bytes(int Dk, int Dv, bool bf16, bool bwd) {
     const DeltaScratch s = delta_scratch(Dk, Dv, bf16);
@@ -146,8 +147,17 @@ __device__ __forceinline__ void values_of(const bf16x8& f, f32x4& x, f32x4& y) {
 __device__ __forceinline__ void values_of(const F32Frag& f, f32x4& x, f32x4& y) { x = f.a; y = f.b; }
 // what rounding to the operand's type loses of x, y, as an operand (bf16: 16 bits of the significand together)
 __device__ __forceinline__ bf16x8 rest_of(const bf16x8& f, const f32x4& x, const f32x4& y) {
+    Frag h;
+    h.v = f;
     f32x4 a, b;
-    values_of(f, a, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {          // (from the packed words: the compiler would convert each value again)
+        unsigned word = h.u[i];
+        asm("" : "+v"(word));
+        f32x4& r = i < 2 ? a : b;
+        r[2 * (i & 1)] = __uint_as_float(word << 16);
+        r[2 * (i & 1) + 1] = __uint_as_float(word & 0xffff0000u);
+    }
     return frag_of<__bf16>(x - a, y - b);
 }
 
@@ -165,49 +175,106 @@ template <int COLS> struct Tile<float, COLS> {
     static __device__ __forceinline__ int at(int r, int c) { return r * RB + c * 4; }
 };
 
-// Eight elements of row `row` from column 32 kb + 8 (lane / 16) on:
-template <class T, int COLS> __device__ __forceinline__ typename El<T>::F row_frag(const char* tile, int row, int kb, int lane) {
-    if constexpr (sizeof(T) == 2) return *(const bf16x8*)(tile + Tile<T, COLS>::chunk(row, 4 * kb + (lane >> 4)));
-    else return *(const F32Frag*)(tile + Tile<T, COLS>::chunk(row, 8 * kb + 2 * (lane >> 4)));
-}
 // Rows (or columns) of a 16-wide tile whose results, with those of the next tile, are eight consecutive ones in a lane:
 // row m of tile t is 32 (t / 2) + 4 (t % 2) + 8 (m / 4) + m % 4; the lane then holds 32 (t / 2) + 8 (lane / 16) + 4 (t % 2) .. +3.
 __device__ __forceinline__ int paired(int t, int m) { return 32 * (t >> 1) + 4 * (t & 1) + 8 * (m >> 2) + (m & 3); }
 
+// Operands from tiles, by LDS byte address.  A reader holds a lane's address in a tile at `lds` and serves every tile of its
+// width that begins a multiple of 1 KB behind: `tile` (a constant) goes into the instruction, and columns into an exclusive
+// or, as the swizzle is one.  hide() keeps the compiler from forming all those addresses ahead of a loop, in registers.
+#ifdef __HIP_DEVICE_COMPILE__
+template <class U> __device__ __forceinline__ U lds_read(unsigned at) { return *(const __attribute__((address_space(3))) U*)at; }
+template <class U> __device__ __forceinline__ void lds_write(unsigned at, const U& x) { *(__attribute__((address_space(3))) U*)at = x; }
+__device__ __forceinline__ s16x4 lds_read_tr(unsigned at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)at);
+}
+#else                                      // (host code has no such addresses)
+template <class U> __device__ U lds_read(unsigned);
+template <class U> __device__ void lds_write(unsigned, const U&);
+__device__ s16x4 lds_read_tr(unsigned);
+#endif
+template <class T> __device__ __forceinline__ typename El<T>::F lds_frag(unsigned at) {
+    if constexpr (sizeof(T) == 2) return lds_read<bf16x8>(at);
+    else return F32Frag{lds_read<f32x4>(at), lds_read<f32x4>(at + 16)};
+}
+// (element by element: a vector of four equal factors would be kept in registers of its own)
+__device__ __forceinline__ f32x4 times(const f32x4& x, float s) { return f32x4{x[0] * s, x[1] * s, x[2] * s, x[3] * s}; }
+__device__ __forceinline__ unsigned hide(unsigned x) {
+    asm("" : "+v"(x));
+    return x;
+}
+
+// Eight elements of one row, from column 32 kb + 8 (lane / 16) on.
+template <class T, int COLS> struct RowReader {
+    unsigned b;
+    __device__ __forceinline__ RowReader(unsigned lds, int row, int lane)
+        : b(lds + Tile<T, COLS>::chunk(row, (sizeof(T) == 2 ? 1 : 2) * (lane >> 4))) {}
+    __device__ __forceinline__ typename El<T>::F frag(int tile, int kb) const {
+        return lds_frag<T>(sizeof(T) == 2 ? (b ^ (kb << 6)) + tile : b + tile + kb * 128);
+    }
+};
+// The same of rows paired(rt, lane % 16)
+template <class T, int COLS> struct PairedRowReader {
+    unsigned even, odd;
+    __device__ __forceinline__ PairedRowReader(unsigned lds, int lane)
+        : even(RowReader<T, COLS>(lds, paired(0, lane & 15), lane).b), odd(RowReader<T, COLS>(lds, paired(1, lane & 15), lane).b) {}
+    __device__ __forceinline__ typename El<T>::F frag(int tile, int rt, int kb) const {
+        RowReader<T, COLS> r = {0, 0, 0};
+        r.b = rt & 1 ? odd : even;
+        return r.frag(tile + (rt >> 1) * 32 * Tile<T, COLS>::RB, kb);
+    }
+};
 // Rows 32 kb + 8 (lane / 16) .. +7 of one column: of column 16 t + lane % 16, or of column paired(t, lane % 16).
-template <class T, int COLS, bool PAIRED> __device__ __forceinline__ typename El<T>::F col_frag(const char* tile, int kb, int t, int lane) {
-    const int row = kb * 32 + 8 * (lane >> 4), s = lane & 15;
-    if constexpr (sizeof(T) == 2) {
-        const int c = PAIRED ? 32 * (t >> 1) + 4 * (t & 1) + 8 * (s & 3) : 16 * t + 4 * (s & 3);
-        Frag f;
-        f.h[0] = lds_tr16(tile + Tile<T, COLS>::at(row + (s >> 2), c));
-        f.h[1] = lds_tr16(tile + Tile<T, COLS>::at(row + 4 + (s >> 2), c));
-        return f.v;
-    } else {
-        const float* p = (const float*)(tile + Tile<T, COLS>::at(row, PAIRED ? paired(t, s) : 16 * t + s));
-        constexpr int LD = Tile<T, COLS>::RB / 4;
-        F32Frag f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f.a[j] = p[j * LD];
-            f.b[j] = p[(4 + j) * LD];
+template <class T, int COLS, bool PAIRED> struct ColReader {
+    unsigned lo, hi;                       // bf16: rows of either half
+    __device__ __forceinline__ ColReader(unsigned lds, int lane) {
+        const int row = 8 * (lane >> 4), s = lane & 15;
+        if constexpr (sizeof(T) == 2) {
+            const int c = (PAIRED ? 8 : 4) * (s & 3);
+            lo = lds + Tile<T, COLS>::at(row + (s >> 2), c);
+            hi = lds + Tile<T, COLS>::at(row + 4 + (s >> 2), c);
+        } else {
+            lo = hi = lds + Tile<T, COLS>::at(row, PAIRED ? paired(0, s) : s);
         }
-        return f;
     }
-}
-// Rows 32 (rt / 2) + 8 (lane / 16) + 4 (rt % 2) .. +3 of column c0 + lane % 16, as fp32
-template <class T, int COLS> __device__ __forceinline__ f32x4 col_values(const char* tile, int rt, int c0, int lane) {
-    const int row = 32 * (rt >> 1) + 8 * (lane >> 4) + 4 * (rt & 1), s = lane & 15;
-    if constexpr (sizeof(T) == 2) {
-        Frag f;
-        f.h[0] = lds_tr16(tile + Tile<T, COLS>::at(row + (s >> 2), c0 + 4 * (s & 3)));
-        return __builtin_convertvector(f.b[0], f32x4);
-    } else {
-        const float* p = (const float*)(tile + Tile<T, COLS>::at(row, c0 + s));
-        constexpr int LD = Tile<T, COLS>::RB / 4;
-        return f32x4{p[0], p[LD], p[2 * LD], p[3 * LD]};
+    __device__ __forceinline__ void hide_all() {
+        lo = hide(lo);
+        if constexpr (sizeof(T) == 2) hi = hide(hi);
     }
-}
+    __device__ __forceinline__ typename El<T>::F frag(int tile, int kb, int t) const {
+        const int at = tile + kb * 32 * Tile<T, COLS>::RB;
+        if constexpr (sizeof(T) == 2) {
+            const int x = PAIRED ? (t >> 1) << 6 : t << 5, y = PAIRED ? (t & 1) * 8 : 0;
+            Frag f;
+            f.h[0] = lds_read_tr((lo ^ x) + at + y);
+            f.h[1] = lds_read_tr((hi ^ x) + at + y);
+            return f.v;
+        } else {
+            const int y = at + 4 * (PAIRED ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t);
+            F32Frag f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f.a[j] = lds_read<float>(lo + y + j * Tile<T, COLS>::RB);
+                f.b[j] = lds_read<float>(lo + y + (4 + j) * Tile<T, COLS>::RB);
+            }
+            return f;
+        }
+    }
+    // rows 32 (rt / 2) + 8 (lane / 16) + 4 (rt % 2) .. +3 of column 16 t + lane % 16, as fp32 (not paired)
+    __device__ __forceinline__ f32x4 values(int tile, int rt, int t) const {
+        const int at = tile + (rt >> 1) * 32 * Tile<T, COLS>::RB;
+        if constexpr (sizeof(T) == 2) {
+            Frag f;
+            f.h[0] = lds_read_tr(((rt & 1 ? hi : lo) ^ (t << 5)) + at);
+            return __builtin_convertvector(f.b[0], f32x4);
+        } else {
+            f32x4 x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = lds_read<float>(lo + at + 64 * t + (4 * (rt & 1) + j) * Tile<T, COLS>::RB);
+            return x;
+        }
+    }
+};
 
 // A tile from global memory, rows `pitch` bytes apart, by W waves; rows from `valid` on become zero.  bf16: fetch() issues
 // direct loads to LDS and the data is there once they have been waited for.  fp32: fetch() loads registers, put() stores them.
@@ -216,21 +283,31 @@ template <int COLS, int W, int ROWS> struct TileFetch<__bf16, COLS, W, ROWS> {
     typedef Swz<COLS> S;
     static constexpr int NV = S::CPR / 4, NI = S::NI * ROWS / kChunk, PER = NI / W;      // loads of a tile and of a wave
     static_assert(NI % W == 0 && NV >= 1, "every wave issues the same number of loads");
-    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, char* tile, int w, int lane) {
-        const unsigned lds = lds_address(tile);
+    // src: wave-uniform
+    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, unsigned lds, int w, int lane) {
+        const int own = (int)hide((unsigned)lane);     // (offsets formed at each fetch: registers are dearer from chunk to chunk)
+        if (valid >= ROWS) {               // a scalar base and the lane's offset, the same for each load where its rows are 16 n apart
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                constexpr int STEP = W * 64 / S::CPR, APART = STEP % 16 ? 16 / STEP : 1;
+                const int j = w + W * (i % APART), slot = 64 * j + own, r = slot / S::CPR, c = (slot % S::CPR) ^ S::key(r);
+                dma16s<false>(lds + 1024u * (unsigned)(w + W * i), src + (size_t)(i / APART * APART * STEP) * pitch, r * pitch + c * 16);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int j = w + W * i, slot = 64 * j + lane, r = slot / S::CPR, c = (slot % S::CPR) ^ S::key(r);
+            const int j = w + W * i, slot = 64 * j + own, r = slot / S::CPR, c = (slot % S::CPR) ^ S::key(r);
             const char* g = src + (size_t)r * pitch + c * 16;
             dma16(lds + 1024u * (unsigned)j, r < valid ? g : (const char*)kZeros);
         }
     }
-    __device__ __forceinline__ void put(char*, int, int) const {}
+    __device__ __forceinline__ void put(unsigned, int, int) const {}
 };
 template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
     static constexpr int CPR = COLS / 4, PER = ROWS * CPR / (64 * W);
     u32x4 v[PER];
-    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, char*, int w, int lane) {
+    __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, unsigned, int w, int lane) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int j = 64 * (w + W * i) + lane, r = j / CPR;
@@ -238,11 +315,11 @@ template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
             if (r < valid) v[i] = *(const u32x4*)(src + (size_t)r * pitch + j % CPR * 16);
         }
     }
-    __device__ __forceinline__ void put(char* tile, int w, int lane) const {
+    __device__ __forceinline__ void put(unsigned lds, int w, int lane) const {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int j = 64 * (w + W * i) + lane;
-            *(u32x4*)(tile + Tile<float, COLS>::chunk(j / CPR, j % CPR)) = v[i];
+            lds_write(lds + Tile<float, COLS>::chunk(j / CPR, j % CPR), v[i]);
         }
     }
 };
@@ -250,24 +327,6 @@ template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
 // ---- plain padded tiles of LD elements a row (the kernels that are not sweeps)
 template <class T, int LD> __device__ __forceinline__ typename El<T>::F row_frag_p(const T* tile, int row, int kb, int lane) {
     return *(const typename El<T>::F*)(tile + row * LD + kb * 32 + 8 * (lane >> 4));
-}
-template <int LD> __device__ __forceinline__ bf16x8 col_frag_p(const __bf16* tile, int kb, int t, int lane) {
-    const int s = lane & 15;
-    const char* p = (const char*)(tile + (kb * 32 + 8 * (lane >> 4) + (s >> 2)) * LD + 16 * t + 4 * (s & 3));
-    Frag f;
-    f.h[0] = lds_tr16(p);
-    f.h[1] = lds_tr16(p + 4 * LD * sizeof(__bf16));
-    return f.v;
-}
-template <int LD> __device__ __forceinline__ F32Frag col_frag_p(const float* tile, int kb, int t, int lane) {
-    const float* p = tile + (kb * 32 + 8 * (lane >> 4)) * LD + 16 * t + (lane & 15);
-    F32Frag f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        f.a[j] = p[j * LD];
-        f.b[j] = p[(4 + j) * LD];
-    }
-    return f;
 }
 
 // COLS columns of `rows` (at most 64) rows, global -> LDS, by THREADS threads; the tile's other rows become zero.

@@ -1,19 +1,16 @@
 // Gated delta rule: the gradients of a chunk of 64 tokens and a head of keys (ltn_delta.h has the formulas), from Z, dY and
 // the states that the sweeps left.  The value heads that share the keys follow one another in one workgroup: their dq and
-// dk are summed in registers, in a fixed order.  Wave w owns tokens 16 w .. +15; the value features come in slabs of VS.
+// dk are summed in registers, in a fixed order.  Wave w owns tokens 16 (w % 4) .. +15 and half of the
+// key features; the value features come in slabs of VS, so that
+// two workgroups fit a compute unit and one's loads pass while the other computes.
 // Scales of rows and columns (decays, beta) are applied to products' fp32 results, never to an operand.
 #include "ltn_delta.h"
 
 namespace ltn {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
-__device__ __forceinline__ float sum16(float x) {          // over the 16 lanes of a row of results
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) x += __shfl_xor(x, d, 64);
-    return x;
-}
 template <class T> __device__ __forceinline__ float dot8(const typename El<T>::F& a, const typename El<T>::F& b) {
     f32x4 a0, a1, b0, b1;
     values_of(a, a0, a1);
@@ -23,228 +20,263 @@ template <class T> __device__ __forceinline__ float dot8(const typename El<T>::F
     for (int i = 0; i < 4; ++i) s = fmaf(a0[i], b0[i], fmaf(a1[i], b1[i], s));
     return s;
 }
-
-template <class T, int DK, int VS>
-struct GradLds {
-    static constexpr int LD = DK + El<T>::PAD, LT = kChunk + El<T>::PAD, LV = VS + El<T>::PAD;
-    T K[kChunk * LD], Q[kChunk * LD];
-    union {
-        struct { T G[kChunk * LV], Z[VS * LT], Y[VS * LT], S[VS * LD], D[VS * LD]; } slab;
-        struct { T dP[kChunk * LT], E[kChunk * LT]; } chunk;
-    };
-    double Gs[kChunk];
-    float gam[kChunk], end[kChunk], beta[kChunk], row[kChunk], col[4][kChunk], part[4];
-};
-
-// rows (at most 64 of them hold data) of COLS elements, contiguous in memory
-template <class T, int LD, int ROWS, int COLS>
-__device__ __forceinline__ void load_rows(T* tile, const T* src, int tid) {
-    constexpr int V = 16 / sizeof(T), PER = COLS / V;
-    for (int i = tid; i < ROWS * PER; i += kThreads) {
-        const int r = i / PER, c = i % PER * V;
-        *(u32x4*)(tile + r * LD + c) = *(const u32x4*)(src + (size_t)r * COLS + c);
-    }
+__device__ __forceinline__ float row_sum16(float x) {      // over the 16 lanes of a row, by rotations within it
+#define LTN_ROTATE(n) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + n, 0xf, 0xf, false))
+    LTN_ROTATE(8);
+    LTN_ROTATE(4);
+    LTN_ROTATE(2);
+    LTN_ROTATE(1);
+#undef LTN_ROTATE
+    return x;
+}
+// four elements in LDS times x; four values to LDS
+template <class T> __device__ __forceinline__ float dot4(unsigned at, const f32x4& x) {
+    f32x4 v;
+    if constexpr (sizeof(T) == 2) v = __builtin_convertvector(lds_read<bf16x4>(at), f32x4);
+    else v = lds_read<f32x4>(at);
+    return v[0] * x[0] + v[1] * x[1] + v[2] * x[2] + v[3] * x[3];
+}
+template <class T> __device__ __forceinline__ void write4(unsigned at, const f32x4& x) {
+    if constexpr (sizeof(T) == 2) lds_write(at, to_bf16(x));
+    else lds_write(at, x);
+}
+// NT tiles of 16 features of the lane's token
+template <int NT> __device__ __forceinline__ void store_row(__bf16* row, const f32x4 (&x)[NT], int grp, bool there) {
+    store_strip<NT>(x, (char*)(row + 8 * grp), there);
+}
+template <int NT> __device__ __forceinline__ void store_row(float* row, const f32x4 (&x)[NT], int grp, bool there) {
+    if (there)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) *(f32x4*)(row + 16 * t + 4 * grp) = x[t];
 }
 
-template <class T, int DK, int VS>
-__global__ __launch_bounds__(kThreads)
+// Two regions: the slab's states, later K and Q; the slab's dO, Z and dY, later dP and E.
+template <class T, int DK, int VS> struct GradLds {
+    static constexpr int GB = Tile<T, VS>::BYTES, ZB = Tile<T, kChunk>::RB * VS, SB = Tile<T, DK>::RB * VS;
+    static constexpr int KB = Tile<T, DK>::BYTES, PB = Tile<T, kChunk>::BYTES;
+    static constexpr int A = 2 * (SB > KB ? SB : KB), B = GB + 2 * ZB > 2 * PB ? GB + 2 * ZB : 2 * PB;
+    static constexpr int S = 0, D = SB, K = 0, Q = KB, G = A, Z = A + GB, Y = A + GB + ZB, P = A, E = A + PB, BYTES = A + B;
+};
+
+// ONE: no other value head shares the keys.
+// All products are taken transposed: a lane's results are four features (or columns) of one token, 16 tok + lane % 16.  Of
+// dO Z^T and dY Z^T the waves of the first half take one, those of the second the other.
+template <class T, int DK, int VS, bool ONE>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2)
 void delta_grad_kernel(DeltaArgs a, int Dv) {
-    typedef GradLds<T, DK, VS> Lds;
+    typedef GradLds<T, DK, VS> L;
     typedef typename El<T>::F F;
-    constexpr int LD = Lds::LD, LT = Lds::LT, LV = Lds::LV, NT = DK / 16;
-    __shared__ __attribute__((aligned(16))) char raw[sizeof(Lds)];
-    Lds& l = *(Lds*)raw;
-    const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = a.H / a.Hk;
+    constexpr int NT = DK / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[L::BYTES];
+    __shared__ __attribute__((aligned(16))) float vec[kVec];             // gam, end, beta, G in two parts
+    __shared__ float row_of[2][kChunk], col_of[kWaves][kChunk], part[kWaves];
+    const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = ONE ? 1 : a.H / a.Hk;
     DeltaSeq s;
     int chunk;
     if (!delta_find(a, slot, s, chunk)) return;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m = lane & 15, grp = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
     const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
+    const int tok = w & 3, hf = w >> 2, r = 16 * tok + m, f0 = hf * NT;    // f0: first of the wave's tiles of 16 key features
     const size_t key_row = ((size_t)s.row * a.Hk + hk) * a.N + s.first + t0;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    const unsigned base = lds_address(lds);
+    const RowReader<T, VS> row_v(base, r, lane);
+    const RowReader<T, kChunk> row_c(base, r, lane);
+    ColReader<T, kChunk, false> col_c(base, lane);
+    ColReader<T, DK, false> col_k(base, lane);
 
-    load_tile<T, LD, DK, kThreads>(l.K, (const T*)a.k + key_row * DK, DK, rows, tid);
-    load_tile<T, LD, DK, kThreads>(l.Q, (const T*)a.q + key_row * DK, DK, rows, tid);
-    f32x4 dq[NT], dk[NT];
+    f32x4 dq[ONE ? 1 : NT], dk[ONE ? 1 : NT];
+    if constexpr (!ONE)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) dq[t] = dk[t] = zero;
+        for (int t = 0; t < NT; ++t) dq[t] = dk[t] = zero;
 
     for (int j = 0; j < group; ++j) {
         const int h = hk * group + j;
         const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first + t0, at = (size_t)slot * a.H + h;
-        if (w == 0) {
-            double x = 0.0;
-            if (lane < rows) {
-                const float gl = a.g[val_row + lane];
-                x = gl < -200.f ? -200.0 : (double)gl;                   // (as for T' and P)
-            }
+        const float mine = threadIdx.x < kVec ? a.vec[at * kVec + threadIdx.x] : 0.f;
+        f32x4 pe[4], qs[NT], ks[NT], ke[NT];
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const double y = __shfl_up(x, d, 64);
-                if (lane >= d) x += y;
-            }
-            l.Gs[lane] = x;
-            l.beta[lane] = lane < rows ? a.beta[val_row + lane] : 0.f;
-            l.gam[lane] = a.vec[at * 3 * kChunk + lane];
-            l.end[lane] = a.vec[at * 3 * kChunk + kChunk + lane];
-        }
-        f32x4 dP[4], E[4], qs[NT], ks[NT], ke[NT];
-#pragma unroll
-        for (int ct = 0; ct < 4; ++ct) dP[ct] = E[ct] = zero;
+        for (int ct = 0; ct < 4; ++ct) pe[ct] = zero;
 #pragma unroll
         for (int t = 0; t < NT; ++t) qs[t] = ks[t] = ke[t] = zero;
         float sdot = 0.f, db = 0.f;
         for (int v0 = 0; v0 < Dv; v0 += VS) {
-            __syncthreads();               // (the tiles' last readers are done; the first time: K, Q and the gates are there)
-            load_tile<T, LV, VS, kThreads>(l.slab.G, (const T*)a.d_o + val_row * Dv + v0, Dv, rows, tid);
-            load_rows<T, LT, VS, kChunk>(l.slab.Z, (const T*)a.z + (at * Dv + v0) * kChunk, tid);
-            load_rows<T, LT, VS, kChunk>(l.slab.Y, (const T*)a.dy + (at * Dv + v0) * kChunk, tid);
-            load_rows<T, LD, VS, DK>(l.slab.S, (const T*)a.s0 + (at * Dv + v0) * DK, tid);
-            load_rows<T, LD, VS, DK>(l.slab.D, (const T*)a.ds + (at * Dv + v0) * DK, tid);
+            TileFetch<T, VS, kWaves> g;
+            TileFetch<T, kChunk, kWaves, VS> z, y;
+            TileFetch<T, DK, kWaves, VS> st, d;
+            if (j || v0) __syncthreads();                                // the tiles' last readers are done
+            z.fetch((const char*)a.z + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, base + L::Z, w, lane);
+            y.fetch((const char*)a.dy + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, base + L::Y, w, lane);
+            g.fetch((const char*)a.d_o + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, base + L::G, w, lane);
+            st.fetch((const char*)a.s0 + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::S, w, lane);
+            d.fetch((const char*)a.ds + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::D, w, lane);
+            if constexpr (sizeof(T) == 2) wait_dma<0>();
+            z.put(base + L::Z, w, lane);
+            y.put(base + L::Y, w, lane);
+            g.put(base + L::G, w, lane);
+            st.put(base + L::S, w, lane);
+            d.put(base + L::D, w, lane);
+            if (v0 == 0 && threadIdx.x < kVec) vec[threadIdx.x] = mine;
             __syncthreads();
-            for (int i = tid; i < VS * DK / 8; i += kThreads) {
-                const int o = i / (DK / 8) * LD + i % (DK / 8) * 8;
-                sdot += dot8<T>(*(const F*)(l.slab.S + o), *(const F*)(l.slab.D + o));
+            const float beta = vec[2 * kChunk + r];
+            col_c.hide_all();
+            col_k.hide_all();
+            for (int i = threadIdx.x; i < VS * DK / 8; i += kThreads) {  // (both tiles are laid out alike)
+                const int o = Tile<T, DK>::at(i / (DK / 8), i % (DK / 8) * 8);
+                sdot += dot8<T>(lds_frag<T>(base + L::S + o), lds_frag<T>(base + L::D + o));
             }
 #pragma unroll
             for (int kb = 0; kb < VS / 32; ++kb) {
-                const F g = row_frag_p<T, LV>(l.slab.G, 16 * w + m, kb, lane);
-                const F y = col_frag_p<LT>(l.slab.Y, kb, w, lane);
-                const F z = col_frag_p<LT>(l.slab.Z, kb, w, lane);
-                db += dot8<T>(y, z);
-                if (16 * w + m < rows) {
+                const F gf = row_v.frag(L::G, kb);
+                const F yf = col_c.frag(L::Y, kb, tok);
+                const F zf = col_c.frag(L::Z, kb, tok);
+                const F own = hf ? yf : gf;
+                db += dot8<T>(yf, zf);
+                if (!hf && r < rows) {
                     f32x4 y0, y1;
-                    values_of(y, y0, y1);
-                    const float b = l.beta[16 * w + m];
-                    *(F*)((T*)a.dv + (val_row + 16 * w + m) * Dv + v0 + 32 * kb + 8 * grp) = frag_of<T>(b * y0, b * y1);
+                    values_of(yf, y0, y1);
+                    *(F*)((T*)a.dv + (val_row + r) * Dv + v0 + 32 * kb + 8 * grp) = frag_of<T>(times(y0, beta), times(y1, beta));
                 }
 #pragma unroll
-                for (int ct = 0; ct < 4; ++ct) {
-                    if (ct > w) continue;
-                    const F b = col_frag_p<LT>(l.slab.Z, kb, ct, lane);
-                    dP[ct] = mma(g, b, dP[ct]);
-                    E[ct] = mma(y, b, E[ct]);
-                }
+                for (int ct = 0; ct < 4; ++ct) pe[ct] = mma(col_c.frag(L::Z, kb, ct), own, pe[ct]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const F b = col_frag_p<LD>(l.slab.S, kb, t, lane), d = col_frag_p<LD>(l.slab.D, kb, t, lane);
-                    qs[t] = mma(g, b, qs[t]);
-                    ks[t] = mma(y, b, ks[t]);
-                    ke[t] = mma(z, d, ke[t]);
+                    const F sf = col_k.frag(L::S, kb, f0 + t), df = col_k.frag(L::D, kb, f0 + t);
+                    qs[t] = mma(sf, gf, qs[t]);
+                    ks[t] = mma(sf, yf, ks[t]);
+                    ke[t] = mma(df, zf, ke[t]);
                 }
             }
         }
+        __syncthreads();                   // the slab is read: K, Q, dP and E take its place
+        TileFetch<T, DK, kWaves> kt, qt;
+        kt.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::K, w, lane);
+        qt.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::Q, w, lane);
         db += __shfl_xor(db, 16, 64);
         db += __shfl_xor(db, 32, 64);
-        if (grp == 0 && 16 * w + m < rows) ((T*)a.dbeta)[val_row + 16 * w + m] = (T)db;
+        if (hf && grp == 0 && r < rows) ((T*)a.dbeta)[val_row + r] = (T)db;
+        {
+            const float beta = vec[2 * kChunk + r], ghi = vec[3 * kChunk + r], glo = vec[4 * kChunk + r], side = hf ? -beta : a.scale;
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) sdot += __shfl_xor(sdot, d, 64);
-        if (lane == 0) l.part[w] = sdot;
-        __syncthreads();                   // the slab is read: dP and E take its place
-
-        const f32x4 gam = *(const f32x4*)(l.gam + 16 * w + 4 * grp), end = *(const f32x4*)(l.end + 16 * w + 4 * grp),
-                    beta = *(const f32x4*)(l.beta + 16 * w + 4 * grp);
-        f32x4 sum = zero, ends = zero;     // of the lane's four rows
+            for (int ct = 0; ct < 4; ++ct) {
+                const int c = 16 * ct + 4 * grp;
+                asm volatile("" : : : "memory");                         // (what it reads would be read for all four ahead)
+                const f32x4 bc = *(const f32x4*)(vec + 2 * kChunk + c), chi = *(const f32x4*)(vec + 3 * kChunk + c),
+                            clo = *(const f32x4*)(vec + 4 * kChunk + c);
+                f32x4& x = pe[ct];
 #pragma unroll
-        for (int ct = 0; ct < 4; ++ct) {
-            const int c = 16 * ct + m;
-            f32x4 kk = zero, qk = zero;
-            if (ct <= w) {
-#pragma unroll
-                for (int kb = 0; kb < DK / 32; ++kb) {
-                    const F b = row_frag_p<T, LD>(l.K, c, kb, lane);
-                    kk = mma(row_frag_p<T, LD>(l.K, 16 * w + m, kb, lane), b, kk);
-                    qk = mma(row_frag_p<T, LD>(l.Q, 16 * w + m, kb, lane), b, qk);
+                for (int i = 0; i < 4; ++i) {
+                    const float y = side * expf((ghi - chi[i]) + (glo - clo[i])) * bc[i] * pe[ct][i];
+                    x[i] = r >= c + i + hf ? y : 0.f;
                 }
+                write4<T>(base + (hf ? L::E : L::P) + Tile<T, kChunk>::at(r, c), x);
             }
-            const double gc = l.Gs[c];
-            const float bc = l.beta[c];
-            float down = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 16 * w + 4 * grp + i;
-                const float ratio = expf((float)(l.Gs[r] - gc)) * bc;
-                const float p = r >= c ? a.scale * ratio * dP[ct][i] : 0.f, e = r > c ? -ratio * beta[i] * E[ct][i] : 0.f;
-                const float both = (r >= c ? p * qk[i] : 0.f) + (r > c ? e * kk[i] : 0.f);
-                sum[i] += both;
-                down += both;
-                l.chunk.dP[r * LT + c] = (T)p;
-                l.chunk.E[r * LT + c] = (T)e;
-            }
-            down += __shfl_xor(down, 16, 64);
-            down += __shfl_xor(down, 32, 64);
-            if (grp == 0) l.col[w][c] = down;
         }
+        const float beta = vec[2 * kChunk + r], gam = vec[r], end = vec[kChunk + r];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            qs[t] *= a.scale * gam;
-            ks[t] *= -gam * beta;
-            ke[t] *= end * beta;
+            qs[t] = times(qs[t], a.scale * gam);
+            ks[t] = times(ks[t], -gam * beta);
+            ke[t] = times(ke[t], end * beta);
+        }
+        if constexpr (sizeof(T) == 2) wait_dma<0>();
+        kt.put(base + L::K, w, lane);
+        qt.put(base + L::Q, w, lane);
+        __syncthreads();
+        float sum = 0.f, last = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int o = (16 * w + 4 * grp + i) * LD + 16 * t + m;
-                const float kv = (float)l.K[o], e = kv * ke[t][i];
-                sum[i] += (float)l.Q[o] * qs[t][i] + kv * ks[t][i] - e;
-                ends[i] += e;
+        for (int t = 0; t < NT; ++t) {
+            const int o = Tile<T, DK>::at(r, 16 * (f0 + t) + 4 * grp);
+            const float e = dot4<T>(base + L::K + o, ke[t]);
+            sum += dot4<T>(base + L::Q + o, qs[t]) + dot4<T>(base + L::K + o, ks[t]) - e;
+            last += e;
+        }
+        {
+            // rows' and columns' sums of dP (.) Q K^T and of E (.) K K^T, from unrounded dP and E: where keys are alike, they
+            // cancel to far less than a rounding of their terms
+            const RowReader<T, DK> own(base + (hf ? L::K : L::Q), r, lane), other(base + L::K, m, lane);
+            f32x4 xk[4];
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct) xk[ct] = zero;
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) {
+                const F b = own.frag(0, kb);
+#pragma unroll
+                for (int ct = 0; ct < 4; ++ct) xk[ct] = mma(other.frag(16 * ct * Tile<T, DK>::RB, kb), b, xk[ct]);
+            }
+#pragma unroll
+            for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float y = r >= 16 * ct + 4 * grp + i + hf ? pe[ct][i] * xk[ct][i] : 0.f, down = row_sum16(y);
+                    sum += y;
+                    if (m == 0) col_of[w][16 * ct + 4 * grp + i] = down;
+                }
+        }
+        col_c.hide_all();
+        col_k.hide_all();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const F pr = row_c.frag(L::P, kb), er = row_c.frag(L::E, kb);
+            const F pc = col_c.frag(L::P, kb, tok), ec = col_c.frag(L::E, kb, tok);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const F kf = col_k.frag(L::K, kb, f0 + t);
+                qs[t] = mma(kf, pr, qs[t]);
+                ks[t] = mma(kf, er, ks[t]);
+                ke[t] = mma(col_k.frag(L::Q, kb, f0 + t), pc, ke[t]);
+                ke[t] = mma(kf, ec, ke[t]);
             }
         }
-        float last = ends[0] + ends[1] + ends[2] + ends[3];
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) last += __shfl_xor(last, d, 64);
+        for (int t = 0; t < NT; ++t) ks[t] += ke[t];
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (grp == 0) row_of[hf][r] = sum;
+        last = fmaf(vec[kChunk - 1], sdot, last);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float x = sum16(sum[i]);
-            if (m == 0) l.row[16 * w + 4 * grp + i] = x;
+        for (int x = 1; x < 64; x *= 2) last += __shfl_xor(last, x, 64);
+        if (lane == 0) part[w] = last;
+        if constexpr (ONE) {
+            store_row<NT>((T*)a.dq + (key_row + r) * DK + 16 * f0, qs, grp, r < rows);
+            store_row<NT>((T*)a.dk + (key_row + r) * DK + 16 * f0, ks, grp, r < rows);
+        } else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                dq[t] += qs[t];
+                dk[t] += ks[t];
+            }
         }
-        if (lane == 0) l.part[w] = l.gam[kChunk - 1] * l.part[w] + last;
         __syncthreads();
         if (w == 0) {
-            float x = l.row[lane] - (l.col[0][lane] + l.col[1][lane] + l.col[2][lane] + l.col[3][lane]);
-            if (lane == 63) x += l.part[0] + l.part[1] + l.part[2] + l.part[3];
+            float x = row_of[0][lane] + row_of[1][lane];
 #pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const float y = __shfl_down(x, d, 64);
-                if (lane + d < 64) x += y;
+            for (int i = 0; i < kWaves; ++i) x -= col_of[i][lane];
+            if (lane == 63)
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) x += part[i];
+#pragma unroll
+            for (int o = 1; o < 64; o *= 2) {
+                const float y = __shfl_down(x, o, 64);
+                if (lane + o < 64) x += y;
             }
             if (lane < rows) ((T*)a.dg)[val_row + lane] = (T)x;
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            f32x4 x = dq[t] + qs[t], y = dk[t] + ks[t] + ke[t];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const F kf = col_frag_p<LD>(l.K, kb, t, lane);
-                if (kb <= w / 2) {
-                    x = mma(row_frag_p<T, LT>(l.chunk.dP, 16 * w + m, kb, lane), kf, x);
-                    y = mma(row_frag_p<T, LT>(l.chunk.E, 16 * w + m, kb, lane), kf, y);
-                }
-                if (kb >= w / 2) {
-                    y = mma(col_frag_p<LT>(l.chunk.dP, kb, w, lane), col_frag_p<LD>(l.Q, kb, t, lane), y);
-                    y = mma(col_frag_p<LT>(l.chunk.E, kb, w, lane), kf, y);
-                }
-            }
-            dq[t] = x;
-            dk[t] = y;
-        }
-        __syncthreads();                   // dP, E and the sums are read: the next head's take their place
+        // (the next head's sums are written behind barriers that wave 0 takes after this)
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 16 * w + 4 * grp + i;
-            if (r < rows) {
-                ((T*)a.dq)[(key_row + r) * DK + 16 * t + m] = (T)dq[t][i];
-                ((T*)a.dk)[(key_row + r) * DK + 16 * t + m] = (T)dk[t][i];
-            }
-        }
+    if constexpr (!ONE) {
+        store_row<NT>((T*)a.dq + (key_row + r) * DK + 16 * f0, dq, grp, r < rows);
+        store_row<NT>((T*)a.dk + (key_row + r) * DK + 16 * f0, dk, grp, r < rows);
+    }
 }
 
 template <class T, int DK, int VS>
 hipError_t launch_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
-    static_assert(sizeof(GradLds<T, DK, VS>) <= 160 * 1024, "LDS");
-    hipLaunchKernelGGL((delta_grad_kernel<T, DK, VS>), dim3((unsigned)((long long)a.slots * a.Hk)), dim3(kThreads), 0, stream, a, Dv);
-    return hipGetLastError();
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.slots * a.Hk)), dim3(kThreads), 0, stream, a, Dv);
+        return hipGetLastError();
+    };
+    return a.H == a.Hk ? launch(delta_grad_kernel<T, DK, VS, true>) : launch(delta_grad_kernel<T, DK, VS, false>);
 }
 
 }  // namespace

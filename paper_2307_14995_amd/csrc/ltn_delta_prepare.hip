@@ -73,10 +73,12 @@ void delta_prepare_kernel(DeltaArgs a) {
         G[lane] = x;
         B[lane] = lane < rows ? a.beta[gate_row + lane] : 0.f;
         const double last = __shfl(x, 63, 64);
-        float* const vec = a.vec + at * 3 * kChunk;
+        float* const vec = a.vec + at * kVec;
         vec[lane] = expf((float)x);
         vec[kChunk + lane] = expf((float)(last - x));
         vec[2 * kChunk + lane] = B[lane];
+        vec[3 * kChunk + lane] = (float)x;
+        vec[4 * kChunk + lane] = (float)(x - (double)(float)x);
     }
     for (int i = tid; i < (BWD ? 2 : 1) * kChunk * LA; i += kThreads) inv[i] = 0.f;
     __syncthreads();

@@ -4,6 +4,9 @@
 // to the accumulators' rows so (paired()) that one product's results are, lane by lane, the next one's right operand:
 // nothing between the products passes through LDS.  What the waves share are the chunk's tiles, the left operands.
 //
+// bf16: the tiles of the next chunk are fetched into a second buffer by a wave that does nothing else.  (The waves that
+// compute spent two thirds of a chunk's 3.7 us on issuing those loads: a wave's next load waits until the memory path has taken the last one.)
+//
 // bf16: S, X, U and T' enter the products of the state in two parts of 8 bits of significand each (three products of
 // four for T' X): the state that the forward hands on is fp32 and stays as exact as sums of fp32 products to some 4e-6;
 // in one part each it would be off by 2.4e-3.  O, rounded to bf16 anyway, takes the larger parts alone.
@@ -20,13 +23,24 @@ template <class T> __device__ __forceinline__ void store_frag(T* p, const typena
 __device__ __forceinline__ void store4(__bf16* p, const f32x4& x) { *(bf16x4*)p = to_bf16(x); }
 __device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 
+// Nothing is scheduled across it (bf16).  Left to itself the compiler reads an operand from LDS right before its product, to
+// save registers that a wave alone on its SIMD has plenty of, and every product waits for LDS.
+template <class T> __device__ __forceinline__ void fence() {
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+}
+
 // One chunk's tiles in LDS.  FWD: K, T', its second part (bf16), V and, where O is wanted, Q and P.  Backward: K, Q, T, P, dO.
 template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
                          T2 = VEC + 1024, Q = T2 + (FWD && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
                          P = Q + (FULL ? Tile<T, DK>::BYTES : 0), BYTES = P + (FULL ? Tile<T, kChunk>::BYTES : 0);
-    static constexpr int BUFS = 2 * BYTES <= 160 * 1024 ? 2 : 1;
+    static constexpr int BUFS = sizeof(T) == 2 ? 2 : 1, ALL = BUFS * BYTES;                   // of a workgroup
+    static_assert(ALL <= 160 * 1024, "LDS");
 };
+
+// Waves that fetch: one besides those that compute (bf16), or all of these (fp32, through registers).
+template <class T> constexpr int fetchers(int W) { return sizeof(T) == 2 ? 1 : W; }
+template <class T> constexpr int threads_of(int W) { return 64 * (sizeof(T) == 2 ? W + 1 : W); }
 
 // The fetches of a chunk's tiles by W waves.
 template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFetch {
@@ -39,7 +53,7 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
     u32x4 vec;
     // at: the chunk's scratch; key_row, val_row: its first token's rows
     __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t at, size_t key_row, size_t val_row, int rows, int Dv, int col0,
-                                          char* lds, int w, int lane) {
+                                          unsigned lds, int w, int lane) {
         k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::K, w, lane);
         t1.fetch((FWD ? a.tq : a.tt) + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T1, w, lane);
         v.fetch((const char*)(FWD ? a.v : a.d_o) + (val_row * Dv + col0) * sizeof(T), Dv * sizeof(T), rows, lds + L::V, w, lane);
@@ -48,13 +62,13 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
             q.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::Q, w, lane);
             p.fetch(a.p + at * kTile, kChunk * sizeof(T), kChunk, lds + L::P, w, lane);
         }
-        if (w == 0) {                      // 768 bytes of decays and beta (the last quarter of the kilobyte is not read)
-            const char* src = (const char*)(a.vec + at * 3 * kChunk) + (lane < 48 ? lane * 16 : 0);
-            if constexpr (BF) dma16(lds_address(lds + L::VEC), src);
+        if (w == 0) {                      // 768 bytes of decays and beta (what else the kilobyte receives is not read)
+            const char* src = (const char*)(a.vec + at * kVec) + (lane < 48 ? lane * 16 : 0);
+            if constexpr (BF) dma16(lds + L::VEC, src);
             else vec = *(const u32x4*)src;
         }
     }
-    __device__ __forceinline__ void put(char* lds, int w, int lane) const {
+    __device__ __forceinline__ void put(unsigned lds, int w, int lane) const {
         if constexpr (!BF) {
             k.put(lds + L::K, w, lane);
             t1.put(lds + L::T1, w, lane);
@@ -63,31 +77,47 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
                 q.put(lds + L::Q, w, lane);
                 p.put(lds + L::P, w, lane);
             }
-            if (w == 0) *(u32x4*)(lds + L::VEC + lane * 16) = vec;
+            if (w == 0) lds_write(lds + L::VEC + lane * 16, vec);
         }
     }
 };
 
 // Forward.  SAVE: Z and the states before chunks are written, for the gradients, and O is not.
 template <class T, int DK, int CT, int W, bool SAVE>
-__global__ __launch_bounds__(64 * W)
+__global__ __launch_bounds__(threads_of<T>(W)) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int COLS = 16 * CT * W, NT = DK / 16;
     typedef typename El<T>::F F;
     typedef SweepLds<T, DK, COLS, !SAVE, true> L;
-    constexpr bool TWO = BF && L::BUFS == 2;
-    __shared__ __attribute__((aligned(1024))) char lds[(TWO ? 2 : 1) * L::BYTES];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];        // (of a size unknown to the compiler, which would else plan for one wave a SIMD and move accumulators to and fro)
 
     int chain, split;
     map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
+    const unsigned lds0 = lds_address(lds);
     const int wg0 = split * COLS, c0 = 16 * CT * w;                      // the workgroup's and the wave's first column
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
 
+    const int chunks = (s.len + kChunk - 1) / kChunk;
+    SweepFetch<T, DK, COLS, fetchers<T>(W), !SAVE, true> next;
+    auto fetch = [&](int chunk) {
+        const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
+        next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
+                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? 0 : w, lane);
+    };
+    if (BF && w == W) {
+        if (chunks) fetch(0);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            wait_dma<0>();
+            __syncthreads();               // this chunk's tiles are there, the last one's are read
+            if (chunk + 1 < chunks) fetch(chunk + 1);
+        }
+        return;
+    }
     f32x4 S[NT][CT];
     {
         const float* in = a.kv_in ? a.kv_in + (size_t)chain * DK * Dv + wg0 + c0 + m : nullptr;
@@ -100,36 +130,35 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 for (int i = 0; i < 4; ++i) S[t][c][i] = in ? in[(size_t)(f + i) * Dv + 16 * c] : 0.f;
             }
     }
-    const int chunks = (s.len + kChunk - 1) / kChunk;
-    SweepFetch<T, DK, COLS, W, !SAVE, true> next;
-    auto fetch = [&](int chunk) {
-        const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
-        next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
-                   lds + (TWO ? (chunk & 1) * L::BYTES : 0), w, lane);
-    };
-    if (chunks) fetch(0);
+    if (!BF && chunks) fetch(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        const char* const cur = lds + (TWO ? (chunk & 1) * L::BYTES : 0);
-        if constexpr (TWO) {
-            wait_dma<0>();
-            __syncthreads();               // this chunk's tiles are there, the last one's are read
-            if (chunk + 1 < chunks) fetch(chunk + 1);
-        } else {
-            if (BF) wait_dma<0>();
-            next.put(lds, w, lane);
-            __syncthreads();
-            if (!BF && chunk + 1 < chunks) fetch(chunk + 1);
-        }
-        const char *const K = cur + L::K, *const Tq = cur + L::T1, *const Tl = cur + L::T2, *const V = cur + L::V,
-                   *const Q = cur + L::Q, *const P = cur + L::P;
-        const float* const vec = (const float*)(cur + L::VEC);           // gam, end, beta
-        const float whole = vec[kChunk - 1];
+        const unsigned base = lds0 + (BF ? (chunk & 1) * L::BYTES : 0);
+        next.put(lds0, w, lane);
+        __syncthreads();
+        if (!BF && chunk + 1 < chunks) fetch(chunk + 1);
+        const PairedRowReader<T, DK> k_row(base, lane);
+        const ColReader<T, DK, true> k_col(base, lane);
+        const PairedRowReader<T, kChunk> t_row(base, lane);
+        const ColReader<T, COLS, false> v_col(base, lane);
+        const RowReader<T, DK> q_row(base, m, lane);
+        const RowReader<T, kChunk> p_row(base, m, lane);
+        constexpr int RD = Tile<T, DK>::RB, RC = Tile<T, kChunk>::RB;
+        const float* const vec = (const float*)(lds + (BF ? (chunk & 1) * L::BYTES : 0) + L::VEC);      // gam, end, beta
+        auto vec4 = [&](int which, int rt) { return *(const f32x4*)(vec + which * kChunk + token_of(rt, grp)); };
 
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             const int col = c0 + 16 * c;
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            F rd[4][NT / 2];               // K's rows, then Q's
+#pragma unroll
+            for (int p = 0; p < NT / 2; ++p)
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) rd[rt][p] = k_row.frag(L::K, rt, p);
+            const float whole = vec[kChunk - 1];
+            fence<T>();
             F Sh[NT / 2], Sl[BF ? NT / 2 : 1];
 #pragma unroll
             for (int p = 0; p < NT / 2; ++p) {
@@ -137,89 +166,124 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p][c], S[2 * p + 1][c]);
                 if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sh[p]);
             }
+            fence<T>();
             f32x4 Z[4], O[4];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] = O[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int p = 0; p < NT / 2; ++p) {
 #pragma unroll
-            for (int p = 0; p < NT / 2; ++p)
+                for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[rt][p], Sh[p], p ? Z[rt] : zero);
+                if constexpr (BF)
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) {
-                    const F kf = row_frag<T, DK>(K, paired(rt, m), p, lane);
-                    Z[rt] = mma(kf, Sh[p], Z[rt]);
-                    if constexpr (BF) Z[rt] = mma(kf, Sl[p], Z[rt]);
-                }
+                    for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[rt][p], Sl[p], Z[rt]);
+            }
+            fence<T>();
+            F tf[6], tl[BF ? 6 : 1];       // T' and its second part: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
+            f32x4 V[4], gam[4];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt)
-                Z[rt] = col_values<T, COLS>(V, rt, col, lane) - *(const f32x4*)(vec + token_of(rt, grp)) * Z[rt];
+            for (int rt = 0; rt < 4; ++rt) {
+                V[rt] = v_col.values(L::V, rt, col / 16);
+                gam[rt] = vec4(0, rt);
+            }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
+                if constexpr (BF) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
+            }
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Z[rt] = V[rt] - gam[rt] * Z[rt];
             F Xh[2], Xl[BF ? 2 : 1];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 Xh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
                 if constexpr (BF) Xl[b] = rest_of(Xh[b], Z[2 * b], Z[2 * b + 1]);
             }
+            fence<T>();
+            f32x4 bt[4], en[4];
+            float row_gam[4];
+            if constexpr (!SAVE)
+#pragma unroll
+                for (int p = 0; p < NT / 2; ++p)
+#pragma unroll
+                    for (int rt = 0; rt < 4; ++rt) rd[rt][p] = q_row.frag(L::Q + 16 * rt * RD, p);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+                bt[rt] = vec4(2, rt);
+                en[rt] = vec4(1, rt);
+                if constexpr (!SAVE) row_gam[rt] = vec[16 * rt + m] * a.scale;
+            }
+            fence<T>();
+#pragma unroll
+            for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
+            if constexpr (BF) {
+#pragma unroll
+                for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xl[i / 4], Z[i < 4 ? i : i - 2]);
+#pragma unroll
+                for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
+            }
             // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory
             if constexpr (!SAVE) {
 #pragma unroll
                 for (int p = 0; p < NT / 2; ++p)
 #pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], row_frag<T, DK>(Q, 16 * rt + m, p, lane), O[rt]);
+                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], rd[rt][p], p ? O[rt] : zero);
             }
+            fence<T>();
+            F kc[2][NT], pf[6];            // K's columns; P's rows
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int t = 0; t < NT; ++t) kc[0][t] = k_col.frag(L::K, 0, t);
+            if constexpr (!SAVE)
 #pragma unroll
-                for (int rt = 2 * b; rt < 4; ++rt) {
-                    const F tf = row_frag<T, kChunk>(Tq, paired(rt, m), b, lane);
-                    Z[rt] = mma(tf, Xh[b], Z[rt]);
-                    if constexpr (BF) {
-                        Z[rt] = mma(tf, Xl[b], Z[rt]);
-                        Z[rt] = mma(row_frag<T, kChunk>(Tl, paired(rt, m), b, lane), Xh[b], Z[rt]);
-                    }
-                }
-            F Uh[2], Ul[BF ? 2 : 1];
+                for (int i = 0; i < 6; ++i) pf[i] = p_row.frag(L::P + 16 * (i < 4 ? i : i - 2) * RC, i / 4);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) kc[1][t] = k_col.frag(L::K, 1, t);
+            fence<T>();
             if constexpr (SAVE) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
                     store_frag<T>((T*)a.z + (at * Dv + wg0 + col + m) * kChunk + 32 * b + 8 * grp, frag_of<T>(Z[2 * b], Z[2 * b + 1]));
             }
+            F Uh[2], Ul[BF ? 2 : 1];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] *= *(const f32x4*)(vec + 2 * kChunk + token_of(rt, grp));    // U
+            for (int rt = 0; rt < 4; ++rt) Z[rt] *= bt[rt];              // U
             if constexpr (!SAVE) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) {
-                    O[rt] *= vec[16 * rt + m] * a.scale;
+                for (int rt = 0; rt < 4; ++rt) O[rt] = times(O[rt], row_gam[rt]);
 #pragma unroll
-                    for (int b = 0; b <= rt / 2; ++b) O[rt] = mma(Uh[b], row_frag<T, kChunk>(P, 16 * rt + m, b, lane), O[rt]);
-                }
+                for (int i = 0; i < 6; ++i) O[i < 4 ? i : i - 2] = mma(Uh[i / 4], pf[i], O[i < 4 ? i : i - 2]);
             }
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] *= *(const f32x4*)(vec + kChunk + token_of(rt, grp));
+            for (int rt = 0; rt < 4; ++rt) Z[rt] *= en[rt];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
                 if constexpr (BF) Ul[b] = rest_of(Uh[b], Z[2 * b], Z[2 * b + 1]);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] *= whole;
+            for (int b = 0; b < 2; ++b) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+                for (int t = 0; t < NT; ++t) S[t][c] = mma(kc[b][t], Uh[b], S[t][c]);
+                if constexpr (BF)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const F kf = col_frag<T, DK, true>(K, b, t, lane);
-                    S[t][c] = mma(kf, Uh[b], S[t][c]);
-                    if constexpr (BF) S[t][c] = mma(kf, Ul[b], S[t][c]);
-                }
+                    for (int t = 0; t < NT; ++t) S[t][c] = mma(kc[b][t], Ul[b], S[t][c]);
+            }
             if constexpr (!SAVE) {
+                T* const out = (T*)a.o + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
+                if (rows == kChunk) {
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt)
-                    if (16 * rt + m < rows) store4((T*)a.o + (val_row + t0 + 16 * rt + m) * Dv + wg0 + col + 4 * grp, O[rt]);
+                    for (int rt = 0; rt < 4; ++rt) store4(out + (size_t)(16 * rt) * Dv, O[rt]);
+                } else {
+#pragma unroll
+                    for (int rt = 0; rt < 4; ++rt)
+                        if (16 * rt + m < rows) store4(out + (size_t)(16 * rt) * Dv, O[rt]);
+                }
             }
         }
-        if constexpr (!TWO) {
-            __syncthreads();
-            if (BF && chunk + 1 < chunks) fetch(chunk + 1);
-        }
+        if constexpr (!BF) __syncthreads();
     }
     if (!SAVE && a.kv_out) {
         float* const out = a.kv_out + (size_t)chain * DK * Dv + wg0 + c0 + m;
@@ -234,20 +298,20 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 
 // Backward, from the last chunk to the first: dY and the derivatives of the states behind chunks.
 template <class T, int DK, int CT, int W>
-__global__ __launch_bounds__(64 * W)
+__global__ __launch_bounds__(threads_of<T>(W)) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int COLS = 16 * CT * W, NT = DK / 16;
     typedef typename El<T>::F F;
     typedef SweepLds<T, DK, COLS, true, false> L;
-    constexpr bool TWO = BF && L::BUFS == 2;
-    __shared__ __attribute__((aligned(1024))) char lds[(TWO ? 2 : 1) * L::BYTES];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
 
     int chain, split;
     map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
+    const unsigned lds0 = lds_address(lds);
     const int wg0 = split * COLS, c0 = 16 * CT * w;
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
@@ -258,87 +322,124 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
         for (int c = 0; c < CT; ++c) S[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int chunks = (s.len + kChunk - 1) / kChunk;
-    SweepFetch<T, DK, COLS, W, true, false> next;
+    SweepFetch<T, DK, COLS, fetchers<T>(W), true, false> next;
     auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
-                   lds + (TWO ? (chunk & 1) * L::BYTES : 0), w, lane);
+                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? 0 : w, lane);
     };
-    if (chunks) fetch(chunks - 1);
-    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-        const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        const char* const cur = lds + (TWO ? (chunk & 1) * L::BYTES : 0);
-        if constexpr (TWO) {
+    if (BF && w == W) {
+        if (chunks) fetch(chunks - 1);
+        for (int chunk = chunks - 1; chunk >= 0; --chunk) {
             wait_dma<0>();
             __syncthreads();
             if (chunk) fetch(chunk - 1);
-        } else {
-            if (BF) wait_dma<0>();
-            next.put(lds, w, lane);
-            __syncthreads();
-            if (!BF && chunk) fetch(chunk - 1);
         }
-        const char *const K = cur + L::K, *const Tt = cur + L::T1, *const G = cur + L::V, *const Q = cur + L::Q, *const P = cur + L::P;
-        const float* const vec = (const float*)(cur + L::VEC);
-        const float whole = vec[kChunk - 1];
+        return;
+    }
+    if (!BF && chunks) fetch(chunks - 1);
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+        const size_t at = (size_t)(s.slot + chunk) * a.H + h;
+        const unsigned base = lds0 + (BF ? (chunk & 1) * L::BYTES : 0);
+        next.put(lds0, w, lane);
+        __syncthreads();
+        if (!BF && chunk) fetch(chunk - 1);
+        const PairedRowReader<T, DK> k_row(base, lane);
+        const ColReader<T, DK, true> k_col(base, lane);
+        const ColReader<T, kChunk, true> t_col(base, lane);
+        const ColReader<T, COLS, false> v_col(base, lane);
+        const float* const vec = (const float*)(lds + (BF ? (chunk & 1) * L::BYTES : 0) + L::VEC);
+        auto vec4 = [&](int which, int rt) { return *(const f32x4*)(vec + which * kChunk + token_of(rt, grp)); };
 
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             const int col = c0 + 16 * c;
+            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+            F rd[4][NT / 2];               // K's rows
+#pragma unroll
+            for (int p = 0; p < NT / 2; ++p)
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) rd[rt][p] = k_row.frag(L::K, rt, p);
+            const float whole = vec[kChunk - 1];
+            fence<T>();
             F Sf[NT / 2];
 #pragma unroll
             for (int p = 0; p < NT / 2; ++p) {
                 Sf[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
                 store_frag<T>((T*)a.ds + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sf[p]);
             }
-            F gf[2];                       // dO
-#pragma unroll
-            for (int b = 0; b < 2; ++b) gf[b] = col_frag<T, COLS, false>(G, b, col / 16, lane);
+            fence<T>();
             f32x4 Y[4];
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Y[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int p = 0; p < NT / 2; ++p)
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(row_frag<T, DK>(K, paired(rt, m), p, lane), Sf[p], Y[rt]);
+                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(rd[rt][p], Sf[p], p ? Y[rt] : zero);
+            fence<T>();
+            // dO's columns; columns of P and T: row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first; columns of Q, later of K
+            F gf[2], pf[6], tf[6], c0f[NT], c1f[NT];
+            f32x4 gam[4], en[4], bt[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) gf[b] = v_col.frag(L::V, b, col / 16);
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
-                Y[rt] *= *(const f32x4*)(vec + kChunk + token_of(rt, grp));
-#pragma unroll
-                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<T, kChunk, true>(P, b, rt, lane), gf[b], Y[rt]);
+                en[rt] = vec4(1, rt);
+                gam[rt] = vec4(0, rt);
             }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) pf[i] = t_col.frag(L::P, i < 4, i < 4 ? i : i - 4);
+#pragma unroll
+            for (int i = 0; i < 6; ++i) tf[i] = t_col.frag(L::T1, i < 4, i < 4 ? i : i - 4);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c0f[t] = k_col.frag(L::Q, 0, t);
+            fence<T>();
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Y[rt] *= en[rt];
+#pragma unroll
+            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
+            F of[2];                       // scale gam dO
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x4 o0, o1;
+                values_of(gf[b], o0, o1);
+                of[b] = frag_of<T>(times(gam[2 * b] * o0, a.scale), times(gam[2 * b + 1] * o1, a.scale));
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c1f[t] = k_col.frag(L::Q, 1, t);
+            fence<T>();
             F uf[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) uf[b] = frag_of<T>(Y[2 * b], Y[2 * b + 1]);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt)
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(c0f[t], of[0], S[t][c]);
 #pragma unroll
-                for (int b = rt / 2; b < 2; ++b) Y[rt] = mma(col_frag<T, kChunk, true>(Tt, b, rt, lane), uf[b], Y[rt]);
-            F xf[2], of[2];                // -gam dV, scale gam dO
+            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(tf[i], uf[i < 4], Y[i < 4 ? i : i - 4]);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c0f[t] = k_col.frag(L::K, 0, t);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(c1f[t], of[1], S[t][c]);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c1f[t] = k_col.frag(L::K, 1, t);
+            fence<T>();
+            F xf[2];                       // -gam dV
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 store_frag<T>((T*)a.dy + (at * Dv + wg0 + col + m) * kChunk + 32 * b + 8 * grp, frag_of<T>(Y[2 * b], Y[2 * b + 1]));
-                const f32x4 g0 = *(const f32x4*)(vec + 32 * b + 8 * grp), g1 = *(const f32x4*)(vec + 32 * b + 8 * grp + 4);
-                const f32x4 b0 = *(const f32x4*)(vec + 2 * kChunk + 32 * b + 8 * grp), b1 = *(const f32x4*)(vec + 2 * kChunk + 32 * b + 8 * grp + 4);
-                xf[b] = frag_of<T>(-g0 * b0 * Y[2 * b], -g1 * b1 * Y[2 * b + 1]);
-                f32x4 o0, o1;
-                values_of(gf[b], o0, o1);
-                of[b] = frag_of<T>(a.scale * g0 * o0, a.scale * g1 * o1);
+                xf[b] = frag_of<T>(-gam[2 * b] * bt[2 * b] * Y[2 * b], -gam[2 * b + 1] * bt[2 * b + 1] * Y[2 * b + 1]);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] *= whole;
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(c0f[t], xf[0], S[t][c]);
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    S[t][c] = mma(col_frag<T, DK, true>(Q, b, t, lane), of[b], S[t][c]);
-                    S[t][c] = mma(col_frag<T, DK, true>(K, b, t, lane), xf[b], S[t][c]);
-                }
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(c1f[t], xf[1], S[t][c]);
         }
-        if constexpr (!TWO) {
-            __syncthreads();
-            if (BF && chunk) fetch(chunk - 1);
-        }
+        if constexpr (!BF) __syncthreads();
     }
 }
 
@@ -346,14 +447,16 @@ template <class T, int DK, bool SAVE>
 hipError_t launch_fwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
     constexpr int CT = 1, W = 4;
     const int per = Dv / (16 * CT * W);
-    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, CT, W, SAVE>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(64 * W), 0, stream, a, Dv, per);
+    typedef SweepLds<T, DK, 16 * CT * W, !SAVE, true> L;
+    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, CT, W, SAVE>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL, stream, a, Dv, per);
     return hipGetLastError();
 }
 template <class T, int DK>
 hipError_t launch_bwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
     constexpr int CT = 1, W = 4;
     const int per = Dv / (16 * CT * W);
-    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, CT, W>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(64 * W), 0, stream, a, Dv, per);
+    typedef SweepLds<T, DK, 16 * CT * W, true, false> L;
+    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, CT, W>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL, stream, a, Dv, per);
     return hipGetLastError();
 }
 
