@@ -209,6 +209,7 @@ template <class T, int COLS> struct RowReader {
     unsigned b;
     __device__ __forceinline__ RowReader(unsigned lds, int row, int lane)
         : b(lds + Tile<T, COLS>::chunk(row, (sizeof(T) == 2 ? 1 : 2) * (lane >> 4))) {}
+    __device__ __forceinline__ void move(int by) { b += by; }
     __device__ __forceinline__ typename El<T>::F frag(int tile, int kb) const {
         return lds_frag<T>(sizeof(T) == 2 ? (b ^ (kb << 6)) + tile : b + tile + kb * 128);
     }
@@ -218,6 +219,10 @@ template <class T, int COLS> struct PairedRowReader {
     unsigned even, odd;
     __device__ __forceinline__ PairedRowReader(unsigned lds, int lane)
         : even(RowReader<T, COLS>(lds, paired(0, lane & 15), lane).b), odd(RowReader<T, COLS>(lds, paired(1, lane & 15), lane).b) {}
+    __device__ __forceinline__ void move(int by) {
+        even += by;
+        odd += by;
+    }
     __device__ __forceinline__ typename El<T>::F frag(int tile, int rt, int kb) const {
         RowReader<T, COLS> r = {0, 0, 0};
         r.b = rt & 1 ? odd : even;
@@ -236,6 +241,10 @@ template <class T, int COLS, bool PAIRED> struct ColReader {
         } else {
             lo = hi = lds + Tile<T, COLS>::at(row, PAIRED ? paired(0, s) : s);
         }
+    }
+    __device__ __forceinline__ void move(int by) {                       // by a multiple of 1 KB
+        lo += by;
+        hi += by;
     }
     __device__ __forceinline__ void hide_all() {
         lo = hide(lo);

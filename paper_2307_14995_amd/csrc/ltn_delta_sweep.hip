@@ -24,7 +24,8 @@ __device__ __forceinline__ void store4(__bf16* p, const f32x4& x) { *(bf16x4*)p 
 __device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 
 // Nothing is scheduled across it (bf16).  Left to itself the compiler reads an operand from LDS right before its product, to
-// save registers that a wave alone on its SIMD has plenty of, and every product waits for LDS.
+// save registers, and every product waits for LDS.  So each read is placed where the registers it goes to have just been
+// used, a stage or more ahead of its own use.
 template <class T> __device__ __forceinline__ void fence() {
     if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
 }
@@ -39,8 +40,9 @@ template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
 };
 
 // Waves that fetch: one besides those that compute (bf16), or all of these (fp32, through registers).
-template <class T> constexpr int fetchers(int W) { return sizeof(T) == 2 ? 1 : W; }
-template <class T> constexpr int threads_of(int W) { return 64 * (sizeof(T) == 2 ? W + 1 : W); }
+constexpr int kFetchers = 4;
+template <class T> constexpr int fetchers(int W) { return sizeof(T) == 2 ? kFetchers : W; }
+template <class T> constexpr int threads_of(int W) { return 64 * (sizeof(T) == 2 ? W + kFetchers : W); }
 
 // The fetches of a chunk's tiles by W waves.
 template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFetch {
@@ -107,9 +109,9 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
-                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? 0 : w, lane);
+                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? w - W : w, lane);
     };
-    if (BF && w == W) {
+    if (BF && w >= W) {
         if (chunks) fetch(0);
         for (int chunk = 0; chunk < chunks; ++chunk) {
             wait_dma<0>();
@@ -119,45 +121,55 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         return;
     }
     f32x4 S[NT][CT];
-    {
-        const float* in = a.kv_in ? a.kv_in + (size_t)chain * DK * Dv + wg0 + c0 + m : nullptr;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) S[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (a.kv_in) {
+        const float* in = a.kv_in + (size_t)chain * DK * Dv + wg0 + c0 + m;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const int f = token_of(t, grp);                          // the same dealing for features
+            for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) S[t][c][i] = in ? in[(size_t)(f + i) * Dv + 16 * c] : 0.f;
-            }
+                for (int i = 0; i < 4; ++i) S[t][c][i] = in[(size_t)(token_of(t, grp) + i) * Dv + 16 * c];   // (features are dealt as tokens)
     }
     if (!BF && chunks) fetch(0);
+    PairedRowReader<T, DK> k_row(lds0, lane);
+    ColReader<T, DK, true> k_col(lds0, lane);
+    PairedRowReader<T, kChunk> t_row(lds0, lane);
+    ColReader<T, COLS, false> v_col(lds0, lane);
+    RowReader<T, DK> q_row(lds0, m, lane);
+    RowReader<T, kChunk> p_row(lds0, m, lane);
+    constexpr int RD = Tile<T, DK>::RB, RC = Tile<T, kChunk>::RB;
+    unsigned vec = lds0 + L::VEC;          // gam, end, beta
+    auto vec4 = [&](int which, int rt) { return lds_read<f32x4>(vec + 32 * grp + 4 * (which * kChunk + token_of(rt, 0))); };
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        const unsigned base = lds0 + (BF ? (chunk & 1) * L::BYTES : 0);
         next.put(lds0, w, lane);
         __syncthreads();
         if (!BF && chunk + 1 < chunks) fetch(chunk + 1);
-        const PairedRowReader<T, DK> k_row(base, lane);
-        const ColReader<T, DK, true> k_col(base, lane);
-        const PairedRowReader<T, kChunk> t_row(base, lane);
-        const ColReader<T, COLS, false> v_col(base, lane);
-        const RowReader<T, DK> q_row(base, m, lane);
-        const RowReader<T, kChunk> p_row(base, m, lane);
-        constexpr int RD = Tile<T, DK>::RB, RC = Tile<T, kChunk>::RB;
-        const float* const vec = (const float*)(lds + (BF ? (chunk & 1) * L::BYTES : 0) + L::VEC);      // gam, end, beta
-        auto vec4 = [&](int which, int rt) { return *(const f32x4*)(vec + which * kChunk + token_of(rt, grp)); };
 
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             const int col = c0 + 16 * c;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            F rd[4][NT / 2];               // K's rows, then Q's
+            F rd[4 * (NT / 2)];            // K's rows, then Q's, then K's columns
+            F tf[6], tl[BF ? 6 : 1], pf[6];        // T' in two parts, P: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
+            f32x4 V[4], gam[4], bt[4], en[4], Z[4], O[4];
+            float row_gam[4];
+            auto k_cols = [&](int i) { return k_col.frag(L::K, i / NT, i % NT); };
 #pragma unroll
-            for (int p = 0; p < NT / 2; ++p)
+            for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
+            const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) rd[rt][p] = k_row.frag(L::K, rt, p);
-            const float whole = vec[kChunk - 1];
+            for (int rt = 0; rt < 4; ++rt) {
+                V[rt] = v_col.values(L::V, rt, col / 16);
+                gam[rt] = vec4(0, rt);
+            }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
             fence<T>();
             F Sh[NT / 2], Sl[BF ? NT / 2 : 1];
 #pragma unroll
@@ -167,28 +179,24 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sh[p]);
             }
             fence<T>();
-            f32x4 Z[4], O[4];
 #pragma unroll
             for (int p = 0; p < NT / 2; ++p) {
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[rt][p], Sh[p], p ? Z[rt] : zero);
+                for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sh[p], p ? Z[rt] : zero);
                 if constexpr (BF)
 #pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[rt][p], Sl[p], Z[rt]);
-            }
-            fence<T>();
-            F tf[6], tl[BF ? 6 : 1];       // T' and its second part: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
-            f32x4 V[4], gam[4];
+                    for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sl[p], Z[rt]);
+                fence<T>();
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                V[rt] = v_col.values(L::V, rt, col / 16);
-                gam[rt] = vec4(0, rt);
+                for (int rt = 0; rt < 4; ++rt) {
+                    if constexpr (SAVE) rd[4 * p + rt] = k_cols(4 * p + rt);
+                    else rd[4 * p + rt] = q_row.frag(L::Q + 16 * rt * RD, p);
+                }
+                fence<T>();
             }
+            if constexpr (BF)
 #pragma unroll
-            for (int i = 0; i < 6; ++i) {
-                tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
-                if constexpr (BF) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
-            }
+                for (int i = 0; i < 6; ++i) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
             fence<T>();
 #pragma unroll
             for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
@@ -201,18 +209,11 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 if constexpr (BF) Xl[b] = rest_of(Xh[b], Z[2 * b], Z[2 * b + 1]);
             }
             fence<T>();
-            f32x4 bt[4], en[4];
-            float row_gam[4];
-            if constexpr (!SAVE)
-#pragma unroll
-                for (int p = 0; p < NT / 2; ++p)
-#pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) rd[rt][p] = q_row.frag(L::Q + 16 * rt * RD, p);
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
                 bt[rt] = vec4(2, rt);
                 en[rt] = vec4(1, rt);
-                if constexpr (!SAVE) row_gam[rt] = vec[16 * rt + m] * a.scale;
+                if constexpr (!SAVE) row_gam[rt] = lds_read<float>(vec + 4 * m + 64 * rt) * a.scale;
             }
             fence<T>();
 #pragma unroll
@@ -223,23 +224,22 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
                 for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
             }
+            fence<T>();
             // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory
             if constexpr (!SAVE) {
 #pragma unroll
-                for (int p = 0; p < NT / 2; ++p)
-#pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], rd[rt][p], p ? O[rt] : zero);
-            }
-            fence<T>();
-            F kc[2][NT], pf[6];            // K's columns; P's rows
-#pragma unroll
-            for (int t = 0; t < NT; ++t) kc[0][t] = k_col.frag(L::K, 0, t);
-            if constexpr (!SAVE)
-#pragma unroll
                 for (int i = 0; i < 6; ++i) pf[i] = p_row.frag(L::P + 16 * (i < 4 ? i : i - 2) * RC, i / 4);
+                fence<T>();
 #pragma unroll
-            for (int t = 0; t < NT; ++t) kc[1][t] = k_col.frag(L::K, 1, t);
-            fence<T>();
+                for (int p = 0; p < NT / 2; ++p) {
+#pragma unroll
+                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], rd[4 * p + rt], p ? O[rt] : zero);
+                    fence<T>();
+#pragma unroll
+                    for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_cols(4 * p + rt);
+                    fence<T>();
+                }
+            }
             if constexpr (SAVE) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
@@ -266,10 +266,10 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) S[t][c] = mma(kc[b][t], Uh[b], S[t][c]);
+                for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], Uh[b], S[t][c]);
                 if constexpr (BF)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t][c] = mma(kc[b][t], Ul[b], S[t][c]);
+                    for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], Ul[b], S[t][c]);
             }
             if constexpr (!SAVE) {
                 T* const out = (T*)a.o + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
@@ -283,7 +283,18 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 }
             }
         }
-        if constexpr (!BF) __syncthreads();
+        if constexpr (BF) {                // the other buffer
+            const int by = chunk & 1 ? -L::BYTES : L::BYTES;
+            k_row.move(by);
+            k_col.move(by);
+            t_row.move(by);
+            v_col.move(by);
+            q_row.move(by);
+            p_row.move(by);
+            vec += by;
+        } else {
+            __syncthreads();
+        }
     }
     if (!SAVE && a.kv_out) {
         float* const out = a.kv_out + (size_t)chain * DK * Dv + wg0 + c0 + m;
@@ -326,9 +337,9 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
-                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? 0 : w, lane);
+                   lds0 + (BF ? (chunk & 1) * L::BYTES : 0), BF ? w - W : w, lane);
     };
-    if (BF && w == W) {
+    if (BF && w >= W) {
         if (chunks) fetch(chunks - 1);
         for (int chunk = chunks - 1; chunk >= 0; --chunk) {
             wait_dma<0>();
@@ -338,46 +349,30 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         return;
     }
     if (!BF && chunks) fetch(chunks - 1);
+    const unsigned first = lds0 + (BF && (chunks - 1) & 1 ? L::BYTES : 0);
+    PairedRowReader<T, DK> k_row(first, lane);
+    ColReader<T, DK, true> k_col(first, lane);
+    ColReader<T, kChunk, true> t_col(first, lane);
+    ColReader<T, COLS, false> v_col(first, lane);
+    unsigned vec = first + L::VEC;
+    auto vec4 = [&](int which, int rt) { return lds_read<f32x4>(vec + 32 * grp + 4 * (which * kChunk + token_of(rt, 0))); };
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
-        const unsigned base = lds0 + (BF ? (chunk & 1) * L::BYTES : 0);
         next.put(lds0, w, lane);
         __syncthreads();
         if (!BF && chunk) fetch(chunk - 1);
-        const PairedRowReader<T, DK> k_row(base, lane);
-        const ColReader<T, DK, true> k_col(base, lane);
-        const ColReader<T, kChunk, true> t_col(base, lane);
-        const ColReader<T, COLS, false> v_col(base, lane);
-        const float* const vec = (const float*)(lds + (BF ? (chunk & 1) * L::BYTES : 0) + L::VEC);
-        auto vec4 = [&](int which, int rt) { return *(const f32x4*)(vec + which * kChunk + token_of(rt, grp)); };
 
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
             const int col = c0 + 16 * c;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            F rd[4][NT / 2];               // K's rows
+            F rd[2 * NT];                  // K's rows, then Q's columns, then K's
+            // dO's columns; columns of P and T: row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first
+            F gf[2], pf[6], tf[6];
+            f32x4 gam[4], en[4], bt[4], Y[4];
 #pragma unroll
-            for (int p = 0; p < NT / 2; ++p)
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) rd[rt][p] = k_row.frag(L::K, rt, p);
-            const float whole = vec[kChunk - 1];
-            fence<T>();
-            F Sf[NT / 2];
-#pragma unroll
-            for (int p = 0; p < NT / 2; ++p) {
-                Sf[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
-                store_frag<T>((T*)a.ds + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sf[p]);
-            }
-            fence<T>();
-            f32x4 Y[4];
-#pragma unroll
-            for (int p = 0; p < NT / 2; ++p)
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(rd[rt][p], Sf[p], p ? Y[rt] : zero);
-            fence<T>();
-            // dO's columns; columns of P and T: row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first; columns of Q, later of K
-            F gf[2], pf[6], tf[6], c0f[NT], c1f[NT];
-            f32x4 gam[4], en[4], bt[4];
+            for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
+            const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
 #pragma unroll
             for (int b = 0; b < 2; ++b) gf[b] = v_col.frag(L::V, b, col / 16);
 #pragma unroll
@@ -387,15 +382,26 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             }
 #pragma unroll
             for (int i = 0; i < 6; ++i) pf[i] = t_col.frag(L::P, i < 4, i < 4 ? i : i - 4);
+            fence<T>();
+            F Sf[NT / 2];
 #pragma unroll
-            for (int i = 0; i < 6; ++i) tf[i] = t_col.frag(L::T1, i < 4, i < 4 ? i : i - 4);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) c0f[t] = k_col.frag(L::Q, 0, t);
+            for (int p = 0; p < NT / 2; ++p) {
+                Sf[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
+                store_frag<T>((T*)a.ds + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sf[p]);
+            }
             fence<T>();
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Y[rt] *= en[rt];
+            for (int p = 0; p < NT / 2; ++p) {
 #pragma unroll
-            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
+                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(rd[4 * p + rt], Sf[p], p ? Y[rt] : zero);
+                fence<T>();
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_col.frag(L::Q, (4 * p + rt) / NT, (4 * p + rt) % NT);
+                fence<T>();
+            }
+#pragma unroll
+            for (int i = 0; i < 6; ++i) tf[i] = t_col.frag(L::T1, i < 4, i < 4 ? i : i - 4);
+            fence<T>();
             F of[2];                       // scale gam dO
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -405,28 +411,31 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             }
 #pragma unroll
             for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Y[rt] *= en[rt];
             fence<T>();
 #pragma unroll
-            for (int t = 0; t < NT; ++t) c1f[t] = k_col.frag(L::Q, 1, t);
+            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[t], of[0], S[t][c]);
+            fence<T>();
+#pragma unroll
+            for (int t = 0; t < NT; ++t) rd[t] = k_col.frag(L::K, 0, t);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
             fence<T>();
             F uf[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) uf[b] = frag_of<T>(Y[2 * b], Y[2 * b + 1]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(c0f[t], of[0], S[t][c]);
-#pragma unroll
             for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(tf[i], uf[i < 4], Y[i < 4 ? i : i - 4]);
             fence<T>();
 #pragma unroll
-            for (int t = 0; t < NT; ++t) c0f[t] = k_col.frag(L::K, 0, t);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
+            for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[NT + t], of[1], S[t][c]);
             fence<T>();
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(c1f[t], of[1], S[t][c]);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) c1f[t] = k_col.frag(L::K, 1, t);
+            for (int t = 0; t < NT; ++t) rd[NT + t] = k_col.frag(L::K, 1, t);
             fence<T>();
             F xf[2];                       // -gam dV
 #pragma unroll
@@ -435,11 +444,20 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 xf[b] = frag_of<T>(-gam[2 * b] * bt[2 * b] * Y[2 * b], -gam[2 * b + 1] * bt[2 * b + 1] * Y[2 * b + 1]);
             }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(c0f[t], xf[0], S[t][c]);
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(c1f[t], xf[1], S[t][c]);
+                for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], xf[b], S[t][c]);
         }
-        if constexpr (!BF) __syncthreads();
+        if constexpr (BF) {
+            const int by = chunk & 1 ? -L::BYTES : L::BYTES;
+            k_row.move(by);
+            k_col.move(by);
+            t_col.move(by);
+            v_col.move(by);
+            vec += by;
+        } else {
+            __syncthreads();
+        }
     }
 }
 
