@@ -12,19 +12,22 @@
 //     X = V - diag(gam) K S0      Z = T' X      U = diag(beta) Z
 //     O = scale diag(gam) Q S0 + P U      S1 = gam_last S0 + K^T diag(end) U
 //
-// and, with dS the derivative by S1 and T = (I + diag(beta) L)^-1,
+// and, with dS the derivative by S1,
 //
-//     dU = P^T dO + diag(end) K dS      dY = T^T dU      dV = diag(beta) dY      dbeta = rows of dY (.) Z
+//     dU = P^T dO + diag(end) K dS      dV = T'^T diag(beta) dU
 //     dS0 = gam_last dS + Q^T diag(scale gam) dO - K^T diag(gam) dV
-//     dP = scale R (.) dO U^T      E = -R (.) diag(beta) dY U^T below the diagonal
-//     dQ = scale diag(gam) dO S0^T + dP K
-//     dK = -diag(gam) dV S0^T + diag(end) U dS^T + dP^T Q + (E + E^T) K
+//     dP = scale R (.) dO Z^T      E = -R (.) dV Z^T below the diagonal      C = diag(end) Z dS^T
+//     dQ = scale diag(gam) dO S0^T + dP diag(beta) K
+//     dK = -diag(gam) dV S0^T + E diag(beta) K + diag(beta) (C + dP^T Q + E^T K)
+//     dbeta_r = k_r . C_r + column r's sum of dP (.) Q K^T + E (.) K K^T
 //     dg_t = sum over r >= t in the chunk of dG_r,
-//     dG_r = q_r . (dQ's first term)_r + k_r . (dK's first term)_r - k_r . (dK's second term)_r
-//            + row r's sums - column r's sums of dP (.) Q K^T and E (.) K K^T,
-//     and dG_last has, besides, the sum of the k . (dK's second term) and gam_last <S0, dS>.
+//     dG_r = q_r . (dQ's first term)_r + k_r . (dK's first term)_r - beta_r dbeta_r + row r's sum of (dP (.) Q K^T + E (.) K K^T) diag(beta),
+//     and dG_last has, besides, gam_last <S0, dS> and the sum of beta_r k_r . C_r
 //
-// Three kinds of kernels: "prepare" (per chunk: T', T, P and the decays; no chunk needs another), "sweeps" (per chain,
+// (dbeta and dg are sums over a token of what its factor, or its exponent, multiplies; T with beta on its other side, and
+// the derivative by U that goes with it, are never formed.)
+//
+// Three kinds of kernels: "prepare" (per chunk: T', P and the decays; no chunk needs another), "sweeps" (per chain,
 // chunk after chunk: the state and what needs it; the columns of S are independent of each other, so value columns are
 // split over waves and workgroups) and "grad" (per chunk, from the states that two sweeps left).
 #pragma once
@@ -47,7 +50,7 @@ struct DeltaArgs {
     long long N;
     float scale;
     // scratch, per (chunk slot, value head): see delta_scratch()
-    char *tq, *tl, *tt, *p, *z, *dy, *s0, *ds;
+    char *tq, *tl, *p, *z, *s0, *ds;
     float* vec;
     int slots;                            // chunk slots of all sequences
 };
@@ -69,13 +72,13 @@ inline DeltaScratch delta_scratch(int Dk, int Dv, bool bf16) {
 }
 inline size_t delta_bytes(int Dk, int Dv, bool bf16, bool bwd) {
     const DeltaScratch s = delta_scratch(Dk, Dv, bf16);
-    // forward: T' (bf16: in two parts), P, decays.  backward: T besides, Z, dY, the states before chunks, their derivatives behind them
-    return (2 + (bf16 ? 1 : 0)) * s.tile + s.vec + (bwd ? s.tile + 2 * s.z + 2 * s.state : 0);
+    // T' (bf16: in two parts), P and decays; for the gradients Z, the states before chunks and their derivatives behind them
+    return (2 + (bf16 ? 1 : 0)) * s.tile + s.vec + (bwd ? s.z + 2 * s.state : 0);
 }
 
 hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_bwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
-hipError_t launch_delta_prepare(const DeltaArgs& a, int Dk, int is_bf16, int is_bwd, hipStream_t stream);
+hipError_t launch_delta_prepare(const DeltaArgs& a, int Dk, int is_bf16, hipStream_t stream);
 hipError_t launch_delta_grad(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);
 // q, k: [chains of Hk, steps, Dk]; v, o: [chains, steps, Dv]; g, beta: [chains, steps]; kv: [chains, Dk, Dv]
 hipError_t launch_delta_decode(const void* q, const void* k, const void* v, void* o, float* kv, const float* g,
@@ -117,12 +120,10 @@ __device__ __forceinline__ bool delta_find(const DeltaArgs& a, int slot, DeltaSe
 template <class T> struct El;
 template <> struct El<__bf16> {
     typedef bf16x8 F;
-    static constexpr int PAD = 8;
 };
 struct F32Frag { f32x4 a, b; };
 template <> struct El<float> {
     typedef F32Frag F;
-    static constexpr int PAD = 4;
 };
 
 __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) { return mfma16(a, b, c); }
@@ -332,23 +333,6 @@ template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
         }
     }
 };
-
-// ---- plain padded tiles of LD elements a row (the kernels that are not sweeps)
-template <class T, int LD> __device__ __forceinline__ typename El<T>::F row_frag_p(const T* tile, int row, int kb, int lane) {
-    return *(const typename El<T>::F*)(tile + row * LD + kb * 32 + 8 * (lane >> 4));
-}
-
-// COLS columns of `rows` (at most 64) rows, global -> LDS, by THREADS threads; the tile's other rows become zero.
-template <class T, int LD, int COLS, int THREADS>
-__device__ __forceinline__ void load_tile(T* tile, const T* src, size_t pitch, int rows, int tid) {
-    constexpr int V = 16 / sizeof(T), PER = COLS / V;
-    for (int i = tid; i < kChunk * PER; i += THREADS) {
-        const int r = i / PER, c = i % PER * V;
-        u32x4 x = {0, 0, 0, 0};
-        if (r < rows) x = *(const u32x4*)(src + (size_t)r * pitch + c);
-        *(u32x4*)(tile + r * LD + c) = x;
-    }
-}
 
 }  // namespace
 }  // namespace ltn

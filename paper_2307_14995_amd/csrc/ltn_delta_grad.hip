@@ -1,4 +1,4 @@
-// Gated delta rule: the gradients of a chunk of 64 tokens and a head of keys (ltn_delta.h has the formulas), from Z, dY and
+// Gated delta rule: the gradients of a chunk of 64 tokens and a head of keys (ltn_delta.h has the formulas), from Z, dV and
 // the states that the sweeps left.  The value heads that share the keys follow one another in one workgroup: their dq and
 // dk are summed in registers, in a fixed order.  Wave w owns tokens 16 (w % 4) .. +15 and half of the
 // key features; the value features come in slabs of VS, so that
@@ -19,6 +19,10 @@ template <class T> __device__ __forceinline__ float dot8(const typename El<T>::F
 #pragma unroll
     for (int i = 0; i < 4; ++i) s = fmaf(a0[i], b0[i], fmaf(a1[i], b1[i], s));
     return s;
+}
+__device__ __forceinline__ float rounded_product(float a, float b) {     // no part of a fused multiply-add
+#pragma clang fp contract(off)
+    return a * b;
 }
 __device__ __forceinline__ float row_sum16(float x) {      // over the 16 lanes of a row, by rotations within it
 #define LTN_ROTATE(n) x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + n, 0xf, 0xf, false))
@@ -50,17 +54,17 @@ template <int NT> __device__ __forceinline__ void store_row(float* row, const f3
         for (int t = 0; t < NT; ++t) *(f32x4*)(row + 16 * t + 4 * grp) = x[t];
 }
 
-// Two regions: the slab's states, later K and Q; the slab's dO, Z and dY, later dP and E.
+// Two regions: the slab's states, later K and Q; the slab's dO, dV and Z, later dP and E.
 template <class T, int DK, int VS> struct GradLds {
     static constexpr int GB = Tile<T, VS>::BYTES, ZB = Tile<T, kChunk>::RB * VS, SB = Tile<T, DK>::RB * VS;
     static constexpr int KB = Tile<T, DK>::BYTES, PB = Tile<T, kChunk>::BYTES;
-    static constexpr int A = 2 * (SB > KB ? SB : KB), B = GB + 2 * ZB > 2 * PB ? GB + 2 * ZB : 2 * PB;
-    static constexpr int S = 0, D = SB, K = 0, Q = KB, G = A, Z = A + GB, Y = A + GB + ZB, P = A, E = A + PB, BYTES = A + B;
+    static constexpr int A = 2 * (SB > KB ? SB : KB), B = 2 * GB + ZB > 2 * PB ? 2 * GB + ZB : 2 * PB;
+    static constexpr int S = 0, D = SB, K = 0, Q = KB, G = A, Y = A + GB, Z = A + 2 * GB, P = A, E = A + PB, BYTES = A + B;
 };
 
 // ONE: no other value head shares the keys.
 // All products are taken transposed: a lane's results are four features (or columns) of one token, 16 tok + lane % 16.  Of
-// dO Z^T and dY Z^T the waves of the first half take one, those of the second the other.
+// dO Z^T and dV Z^T the waves of the first half take one, those of the second the other.
 template <class T, int DK, int VS, bool ONE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2)
 void delta_grad_kernel(DeltaArgs a, int Dv) {
@@ -69,7 +73,7 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
     constexpr int NT = DK / 32;
     __shared__ __attribute__((aligned(1024))) char lds[L::BYTES];
     __shared__ __attribute__((aligned(16))) float vec[kVec];             // gam, end, beta, G in two parts
-    __shared__ float row_of[2][kChunk], col_of[kWaves][kChunk], part[kWaves];
+    __shared__ __attribute__((aligned(16))) float row_of[2][kChunk], end_of[2][kChunk], col_of[kWaves][kChunk], part[kWaves];
     const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = ONE ? 1 : a.H / a.Hk;
     DeltaSeq s;
     int chunk;
@@ -99,14 +103,14 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
         for (int ct = 0; ct < 4; ++ct) pe[ct] = zero;
 #pragma unroll
         for (int t = 0; t < NT; ++t) qs[t] = ks[t] = ke[t] = zero;
-        float sdot = 0.f, db = 0.f;
+        float sdot = 0.f;
         for (int v0 = 0; v0 < Dv; v0 += VS) {
-            TileFetch<T, VS, kWaves> g;
-            TileFetch<T, kChunk, kWaves, VS> z, y;
+            TileFetch<T, VS, kWaves> g, y;
+            TileFetch<T, kChunk, kWaves, VS> z;
             TileFetch<T, DK, kWaves, VS> st, d;
             if (j || v0) __syncthreads();                                // the tiles' last readers are done
             z.fetch((const char*)a.z + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, base + L::Z, w, lane);
-            y.fetch((const char*)a.dy + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, base + L::Y, w, lane);
+            y.fetch((const char*)a.dv + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, base + L::Y, w, lane);
             g.fetch((const char*)a.d_o + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, base + L::G, w, lane);
             st.fetch((const char*)a.s0 + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::S, w, lane);
             d.fetch((const char*)a.ds + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::D, w, lane);
@@ -118,7 +122,6 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             d.put(base + L::D, w, lane);
             if (v0 == 0 && threadIdx.x < kVec) vec[threadIdx.x] = mine;
             __syncthreads();
-            const float beta = vec[2 * kChunk + r];
             col_c.hide_all();
             col_k.hide_all();
             for (int i = threadIdx.x; i < VS * DK / 8; i += kThreads) {  // (both tiles are laid out alike)
@@ -128,15 +131,9 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
 #pragma unroll
             for (int kb = 0; kb < VS / 32; ++kb) {
                 const F gf = row_v.frag(L::G, kb);
-                const F yf = col_c.frag(L::Y, kb, tok);
+                const F yf = row_v.frag(L::Y, kb);
                 const F zf = col_c.frag(L::Z, kb, tok);
                 const F own = hf ? yf : gf;
-                db += dot8<T>(yf, zf);
-                if (!hf && r < rows) {
-                    f32x4 y0, y1;
-                    values_of(yf, y0, y1);
-                    *(F*)((T*)a.dv + (val_row + r) * Dv + v0 + 32 * kb + 8 * grp) = frag_of<T>(times(y0, beta), times(y1, beta));
-                }
 #pragma unroll
                 for (int ct = 0; ct < 4; ++ct) pe[ct] = mma(col_c.frag(L::Z, kb, ct), own, pe[ct]);
 #pragma unroll
@@ -152,11 +149,8 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
         TileFetch<T, DK, kWaves> kt, qt;
         kt.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::K, w, lane);
         qt.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::Q, w, lane);
-        db += __shfl_xor(db, 16, 64);
-        db += __shfl_xor(db, 32, 64);
-        if (hf && grp == 0 && r < rows) ((T*)a.dbeta)[val_row + r] = (T)db;
         {
-            const float beta = vec[2 * kChunk + r], ghi = vec[3 * kChunk + r], glo = vec[4 * kChunk + r], side = hf ? -beta : a.scale;
+            const float ghi = vec[3 * kChunk + r], glo = vec[4 * kChunk + r], side = hf ? -1.f : a.scale;
 #pragma unroll
             for (int ct = 0; ct < 4; ++ct) {
                 const int c = 16 * ct + 4 * grp;
@@ -166,30 +160,30 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
                 f32x4& x = pe[ct];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float y = side * expf((ghi - chi[i]) + (glo - clo[i])) * bc[i] * pe[ct][i];
+                    const float y = side * expf((ghi - chi[i]) + (glo - clo[i])) * pe[ct][i];
                     x[i] = r >= c + i + hf ? y : 0.f;
                 }
-                write4<T>(base + (hf ? L::E : L::P) + Tile<T, kChunk>::at(r, c), x);
+                write4<T>(base + (hf ? L::E : L::P) + Tile<T, kChunk>::at(r, c), x * bc);
             }
         }
         const float beta = vec[2 * kChunk + r], gam = vec[r], end = vec[kChunk + r];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             qs[t] = times(qs[t], a.scale * gam);
-            ks[t] = times(ks[t], -gam * beta);
-            ke[t] = times(ke[t], end * beta);
+            ks[t] = times(ks[t], -gam);
+            ke[t] = times(ke[t], end);
         }
         if constexpr (sizeof(T) == 2) wait_dma<0>();
         kt.put(base + L::K, w, lane);
         qt.put(base + L::Q, w, lane);
         __syncthreads();
-        float sum = 0.f, last = 0.f;
+        float sum = 0.f, ends = 0.f;       // of token r: what its row gives dG; k . C
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int o = Tile<T, DK>::at(r, 16 * (f0 + t) + 4 * grp);
-            const float e = dot4<T>(base + L::K + o, ke[t]);
-            sum += dot4<T>(base + L::Q + o, qs[t]) + dot4<T>(base + L::K + o, ks[t]) - e;
-            last += e;
+            sum += dot4<T>(base + L::Q + o, qs[t]) + dot4<T>(base + L::K + o, ks[t]);
+            ends += dot4<T>(base + L::K + o, ke[t]);
+            ke[t] = times(ke[t], beta);
         }
         {
             // rows' and columns' sums of dP (.) Q K^T and of E (.) K K^T, from unrounded dP and E: where keys are alike, they
@@ -205,13 +199,17 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
                 for (int ct = 0; ct < 4; ++ct) xk[ct] = mma(other.frag(16 * ct * Tile<T, DK>::RB, kb), b, xk[ct]);
             }
 #pragma unroll
-            for (int ct = 0; ct < 4; ++ct)
+            for (int ct = 0; ct < 4; ++ct) {
+                const f32x4 bc = *(const f32x4*)(vec + 2 * kChunk + 16 * ct + 4 * grp);
+                f32x4 down;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float y = r >= 16 * ct + 4 * grp + i + hf ? pe[ct][i] * xk[ct][i] : 0.f, down = row_sum16(y);
-                    sum += y;
-                    if (m == 0) col_of[w][16 * ct + 4 * grp + i] = down;
+                    const float y = r >= 16 * ct + 4 * grp + i + hf ? pe[ct][i] * xk[ct][i] : 0.f;
+                    sum += rounded_product(bc[i], y);
+                    down[i] = row_sum16(y);
                 }
+                if (m == 0) *(f32x4*)(col_of[w] + 16 * ct + 4 * grp) = down;
+            }
         }
         col_c.hide_all();
         col_k.hide_all();
@@ -232,11 +230,15 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
         for (int t = 0; t < NT; ++t) ks[t] += ke[t];
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
-        if (grp == 0) row_of[hf][r] = sum;
-        last = fmaf(vec[kChunk - 1], sdot, last);
+        ends += __shfl_xor(ends, 16, 64);
+        ends += __shfl_xor(ends, 32, 64);
+        if (grp == 0) {
+            row_of[hf][r] = sum;
+            end_of[hf][r] = ends;
+        }
 #pragma unroll
-        for (int x = 1; x < 64; x *= 2) last += __shfl_xor(last, x, 64);
-        if (lane == 0) part[w] = last;
+        for (int x = 1; x < 64; x *= 2) sdot += __shfl_xor(sdot, x, 64);
+        if (lane == 0) part[w] = sdot;
         if constexpr (ONE) {
             store_row<NT>((T*)a.dq + (key_row + r) * DK + 16 * f0, qs, grp, r < rows);
             store_row<NT>((T*)a.dk + (key_row + r) * DK + 16 * f0, ks, grp, r < rows);
@@ -249,12 +251,18 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
         }
         __syncthreads();
         if (w == 0) {
-            float x = row_of[0][lane] + row_of[1][lane];
+            const float bt = vec[2 * kChunk + lane], e = end_of[0][lane] + end_of[1][lane];
+            float d = e, x = row_of[0][lane] + row_of[1][lane], all = bt * e, states = 0.f;
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) x -= col_of[i][lane];
-            if (lane == 63)
+            for (int i = 0; i < kWaves; ++i) {
+                d += col_of[i][lane];
+                states += part[i];
+            }
+            if (lane < rows) ((T*)a.dbeta)[val_row + lane] = (T)d;
+            x -= rounded_product(bt, d);         // (rounded as the rows' terms are: a diagonal's two cancel)
 #pragma unroll
-                for (int i = 0; i < kWaves; ++i) x += part[i];
+            for (int o = 1; o < 64; o *= 2) all += __shfl_xor(all, o, 64);
+            if (lane == 63) x += fmaf(vec[kChunk - 1], states, all);
 #pragma unroll
             for (int o = 1; o < 64; o *= 2) {
                 const float y = __shfl_down(x, o, 64);

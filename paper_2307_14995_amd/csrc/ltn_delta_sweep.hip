@@ -23,6 +23,31 @@ template <class T> __device__ __forceinline__ void store_frag(T* p, const typena
 __device__ __forceinline__ void store4(__bf16* p, const f32x4& x) { *(bf16x4*)p = to_bf16(x); }
 __device__ __forceinline__ void store4(float* p, const f32x4& x) { *(f32x4*)p = x; }
 
+// A wave's 16 columns of 64 tokens, from a column a lane to a token a lane (16 rows of a tile of a wave's own; a wave's
+// accesses to LDS stay in order).
+template <class T> struct Turn {
+    typedef Tile<T, kChunk> Ti;
+    static constexpr int BYTES = 16 * Ti::RB;
+    unsigned in, out;
+    __device__ __forceinline__ Turn(unsigned lds, int lane) {
+        const int m = lane & 15, grp = lane >> 4;
+        in = lds + Ti::chunk(m, sizeof(T) == 2 ? grp : 2 * grp);
+        out = lds + (sizeof(T) == 2 ? Ti::at(4 * grp + (m >> 2), 4 * (m & 3)) : Ti::at(4 * grp, m));
+    }
+    __device__ __forceinline__ void write(int b, const bf16x8& f) const { lds_write(in ^ (b << 6), f); }
+    __device__ __forceinline__ void write(int b, const F32Frag& f) const {
+        lds_write(in + b * 128, f.a);
+        lds_write(in + b * 128 + 16, f.b);
+    }
+    __device__ __forceinline__ void store(__bf16* p, int rt) const { *(s16x4*)p = lds_read_tr(out ^ (rt << 5)); }
+    __device__ __forceinline__ void store(float* p, int rt) const {
+        f32x4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = lds_read<float>(out + 64 * rt + i * Ti::RB);
+        *(f32x4*)p = x;
+    }
+};
+
 // Nothing is scheduled across it (bf16).  Left to itself the compiler reads an operand from LDS right before its product, to
 // save registers, and every product waits for LDS.  So each read is placed where the registers it goes to have just been
 // used, a stage or more ahead of its own use.
@@ -30,7 +55,7 @@ template <class T> __device__ __forceinline__ void fence() {
     if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
 }
 
-// One chunk's tiles in LDS.  FWD: K, T', its second part (bf16), V and, where O is wanted, Q and P.  Backward: K, Q, T, P, dO.
+// One chunk's tiles in LDS.  FWD: K, T', its second part (bf16), V and, where O is wanted, Q and P.  Backward: K, Q, T', P, dO.
 template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
                          T2 = VEC + 1024, Q = T2 + (FWD && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
@@ -57,7 +82,7 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
     __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t at, size_t key_row, size_t val_row, int rows, int Dv, int col0,
                                           unsigned lds, int w, int lane) {
         k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::K, w, lane);
-        t1.fetch((FWD ? a.tq : a.tt) + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T1, w, lane);
+        t1.fetch(a.tq + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T1, w, lane);
         v.fetch((const char*)(FWD ? a.v : a.d_o) + (val_row * Dv + col0) * sizeof(T), Dv * sizeof(T), rows, lds + L::V, w, lane);
         if constexpr (FWD && BF) t2.fetch(a.tl + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T2, w, lane);
         if constexpr (FULL) {
@@ -307,7 +332,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     }
 }
 
-// Backward, from the last chunk to the first: dY and the derivatives of the states behind chunks.
+// Backward, from the last chunk to the first: dV and the derivatives of the states behind chunks.
 template <class T, int DK, int CT, int W>
 __global__ __launch_bounds__(threads_of<T>(W)) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
@@ -356,7 +381,9 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     ColReader<T, COLS, false> v_col(first, lane);
     unsigned vec = first + L::VEC;
     auto vec4 = [&](int which, int rt) { return lds_read<f32x4>(vec + 32 * grp + 4 * (which * kChunk + token_of(rt, 0))); };
+    const Turn<T> turn(lds0 + L::ALL + w * Turn<T>::BYTES, lane);
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+        const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
         next.put(lds0, w, lane);
         __syncthreads();
@@ -367,7 +394,7 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             const int col = c0 + 16 * c;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             F rd[2 * NT];                  // K's rows, then Q's columns, then K's
-            // dO's columns; columns of P and T: row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first
+            // dO's columns; columns of P and T': row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first
             F gf[2], pf[6], tf[6];
             f32x4 gam[4], en[4], bt[4], Y[4];
 #pragma unroll
@@ -418,14 +445,17 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
             fence<T>();
 #pragma unroll
+            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
+            fence<T>();
+#pragma unroll
             for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[t], of[0], S[t][c]);
             fence<T>();
 #pragma unroll
             for (int t = 0; t < NT; ++t) rd[t] = k_col.frag(L::K, 0, t);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
             fence<T>();
             F uf[2];
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Y[rt] *= bt[rt];
 #pragma unroll
             for (int b = 0; b < 2; ++b) uf[b] = frag_of<T>(Y[2 * b], Y[2 * b + 1]);
 #pragma unroll
@@ -437,16 +467,25 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) rd[NT + t] = k_col.frag(L::K, 1, t);
             fence<T>();
+            // dV, turned round in LDS for its rows in memory: written a column a lane, read four columns of a token a lane
+#pragma unroll
+            for (int b = 0; b < 2; ++b) turn.write(b, frag_of<T>(Y[2 * b], Y[2 * b + 1]));
             F xf[2];                       // -gam dV
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                store_frag<T>((T*)a.dy + (at * Dv + wg0 + col + m) * kChunk + 32 * b + 8 * grp, frag_of<T>(Y[2 * b], Y[2 * b + 1]));
-                xf[b] = frag_of<T>(-gam[2 * b] * bt[2 * b] * Y[2 * b], -gam[2 * b + 1] * bt[2 * b + 1] * Y[2 * b + 1]);
-            }
+            for (int b = 0; b < 2; ++b) xf[b] = frag_of<T>(-gam[2 * b] * Y[2 * b], -gam[2 * b + 1] * Y[2 * b + 1]);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], xf[b], S[t][c]);
+            T* const out = (T*)a.dv + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
+            if (rows == kChunk) {
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt) turn.store(out + (size_t)(16 * rt) * Dv, rt);
+            } else {
+#pragma unroll
+                for (int rt = 0; rt < 4; ++rt)
+                    if (16 * rt + m < rows) turn.store(out + (size_t)(16 * rt) * Dv, rt);
+            }
         }
         if constexpr (BF) {
             const int by = chunk & 1 ? -L::BYTES : L::BYTES;
@@ -474,7 +513,7 @@ hipError_t launch_bwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
     constexpr int CT = 1, W = 4;
     const int per = Dv / (16 * CT * W);
     typedef SweepLds<T, DK, 16 * CT * W, true, false> L;
-    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, CT, W>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL, stream, a, Dv, per);
+    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, CT, W>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL + W * Turn<T>::BYTES, stream, a, Dv, per);
     return hipGetLastError();
 }
 
@@ -482,7 +521,7 @@ hipError_t launch_bwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
 
 hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream) {
     if (a.slots > 0) {
-        const hipError_t e = launch_delta_prepare(a, Dk, is_bf16, 0, stream);
+        const hipError_t e = launch_delta_prepare(a, Dk, is_bf16, stream);
         if (e != hipSuccess) return e;
     }
     if (Dk == 64) return is_bf16 ? launch_fwd_t<__bf16, 64, false>(a, Dv, stream) : launch_fwd_t<float, 64, false>(a, Dv, stream);
@@ -490,7 +529,7 @@ hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hip
 }
 
 hipError_t launch_delta_bwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream) {
-    hipError_t e = launch_delta_prepare(a, Dk, is_bf16, 1, stream);
+    hipError_t e = launch_delta_prepare(a, Dk, is_bf16, stream);
     if (e != hipSuccess) return e;
     if (Dk == 64) e = is_bf16 ? launch_fwd_t<__bf16, 64, true>(a, Dv, stream) : launch_fwd_t<float, 64, true>(a, Dv, stream);
     else e = is_bf16 ? launch_fwd_t<__bf16, 128, true>(a, Dv, stream) : launch_fwd_t<float, 128, true>(a, Dv, stream);

@@ -52,9 +52,7 @@ size_t lay_out(ltn::DeltaArgs& a, char* base, int Dk, int Dv, bool bf16, bool bw
     a.p = take(s.tile);
     a.vec = reinterpret_cast<float*>(take(s.vec));
     if (bwd) {
-        a.tt = take(s.tile);
         a.z = take(s.z);
-        a.dy = take(s.z);
         a.s0 = take(s.state);
         a.ds = take(s.state);
     }
