@@ -66,7 +66,7 @@ template <class T, int DK, int VS> struct GradLds {
 // All products are taken transposed: a lane's results are four features (or columns) of one token, 16 tok + lane % 16.  Of
 // dO Z^T and dV Z^T the waves of the first half take one, those of the second the other.
 template <class T, int DK, int VS, bool ONE>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 4 : 2)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && ONE ? 4 : 2)
 void delta_grad_kernel(DeltaArgs a, int Dv) {
     typedef GradLds<T, DK, VS> L;
     typedef typename El<T>::F F;
