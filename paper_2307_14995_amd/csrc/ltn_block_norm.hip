@@ -46,6 +46,24 @@ template <> struct Piece<float> {
 
 enum { kNoGate = 0, kElementGate = 1, kSharedGate = 2 };
 
+// A row's pieces of a lane as they come from memory, and as fp32.
+template <class T, int NP> struct Raw { u32x4 v[NP]; };
+template <class T, int NP> __device__ __forceinline__ void widen(const Raw<T, NP>& r, float* v) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[8 * i + 2 * j] = __uint_as_float(r.v[i][j] << 16);
+                v[8 * i + 2 * j + 1] = __uint_as_float(r.v[i][j] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * i + j] = __uint_as_float(r.v[i][j]);
+        }
+    }
+}
+
 // One team of WPR waves per row.  The lane's piece i of a row begins at column at(i); live(i): it is within the row.
 template <class T, int EL, int WPR, int GATE>
 struct Row {
@@ -67,6 +85,13 @@ struct Row {
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[i * N + j] = other;
             }
+        }
+    }
+    __device__ __forceinline__ void fetch(const T* p, Raw<T, NP>& r) const {               // (zeros behind the row)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            r.v[i] = u32x4{0, 0, 0, 0};
+            if (live(i)) r.v[i] = *(const u32x4*)(p + at(i));
         }
     }
     template <class U> __device__ __forceinline__ void store(U* p, const float* v) const {
@@ -115,7 +140,8 @@ struct NormArgs {
     float scale, eps;
     int after, C;
     long long rows, strip, per_gate;       // rows of a strip; rows that share a gate
-    float* part;                           // [strips][dw_after, dw_before, a gate that began before, one that goes on after][C]
+    float* part;                           // [workgroups][dw_after, dw_before][C]
+    float* gate_part;                      // [strips][a gate that began before, one that goes on after][C]
 };
 
 constexpr int kThreads(int wpr) { return wpr == 8 ? 512 : 256; }
@@ -144,28 +170,43 @@ void block_norm_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < EL; ++i) dg[i] = 0.f;
     }
-    // every team of the workgroup runs the same number of rows: those past the end are not there, but meet at the barriers
-    for (long long n = 0; n < a.strip; ++n) {
+    // every team of the workgroup runs the same number of rows: those past the end are not there, but meet at the barriers.
+    // The next row is fetched while one is worked on: two waves a SIMD, all that the sums' registers leave, would else
+    // have nothing under way half of the time (norm of 32768 x 4096 backward 516 us without).
+    const long long wg_first = (long long)blockIdx.x * TEAMS * a.strip;
+    const long long steps = a.rows - wg_first < a.strip ? a.rows - wg_first : a.strip;
+    Raw<T, R::NP> rx, ry_, rg, rdx, rdh;
+    auto fetch = [&](long long n) {
+        const long long row = first + n < a.rows ? first + n : a.rows - 1;
+        const size_t off = (size_t)row * a.C;
+        r.fetch((const T*)a.x + off, rx);
+        r.fetch((const T*)a.y + off, ry_);
+        if constexpr (GATE == kElementGate) r.fetch((const T*)a.gate + off, rg);
+        if constexpr (GATE == kSharedGate) r.fetch((const T*)a.gate + (size_t)(row / a.per_gate) * a.C, rg);
+        if constexpr (BWD) {
+            if (a.d_x_out) r.fetch((const T*)a.d_x_out + off, rdx);
+            r.fetch((const T*)a.d_h + off, rdh);
+        }
+    };
+    if constexpr (BWD)
+        if (!a.d_x_out)
+#pragma unroll
+            for (int i = 0; i < R::NP; ++i) rdx.v[i] = u32x4{0, 0, 0, 0};
+    if (steps > 0) fetch(0);
+    for (long long n = 0; n < steps; ++n) {
         const long long row = first + n;
         const bool there = row < a.rows;
-        if (WPR == 1 && !there) break;
-        if ((long long)blockIdx.x * TEAMS * a.strip + n >= a.rows) break;        // (none of the workgroup's teams has one)
         const size_t off = (size_t)(there ? row : a.rows - 1) * a.C;
         float x[EL], y[EL], g[GATE ? EL : 1];
-        r.load((const T*)a.x + off, x, 0.f);
-        r.load((const T*)a.y + off, y, 0.f);
-        if constexpr (GATE == kElementGate) r.load((const T*)a.gate + off, g, 0.f);
-        if constexpr (GATE == kSharedGate) r.load((const T*)a.gate + (size_t)((there ? row : a.rows - 1) / a.per_gate) * a.C, g, 0.f);
+        widen(rx, x);
+        widen(ry_, y);
+        if constexpr (GATE) widen(rg, g);
         float dxo[BWD ? EL : 1], dh[BWD ? EL : 1];
         if constexpr (BWD) {
-            if (a.d_x_out) {
-                r.load((const T*)a.d_x_out + off, dxo, 0.f);
-            } else {
-#pragma unroll
-                for (int i = 0; i < EL; ++i) dxo[i] = 0.f;
-            }
-            r.load((const T*)a.d_h + off, dh, 0.f);
+            widen(rdx, dxo);
+            widen(rdh, dh);
         }
+        if (n + 1 < steps) fetch(n + 1);
         float ry = 1.f;
         if (a.after) {
             float ss[1] = {0.f};
@@ -183,22 +224,22 @@ void block_norm_kernel(NormArgs a) {
             if constexpr (BWD) s2[1] = fmaf(dh[i] * wb[i], x[i], s2[1]);
         }
         team_sum<BWD ? 2 : 1, WPR>(*(float(*)[BWD ? 2 : 1])s2, meet, turn, wave);
-        const float rx = 1.f / sqrtf(s2[0] * inv + a.eps);
+        const float rs = 1.f / sqrtf(s2[0] * inv + a.eps);
         if constexpr (!BWD) {
             if (there) {
                 r.store((T*)a.x_out + off, x);
 #pragma unroll
-                for (int i = 0; i < EL; ++i) x[i] *= rx * wb[i];
+                for (int i = 0; i < EL; ++i) x[i] *= rs * wb[i];
                 r.store((T*)a.h + off, x);
             }
         } else {
-            const float c1 = s2[1] * rx * inv;
+            const float c1 = s2[1] * rs * inv;
             float s3[1] = {0.f};
 #pragma unroll
             for (int i = 0; i < EL; ++i) {
-                const float mi = x[i] * rx;
+                const float mi = x[i] * rs;
                 if (there) db[i] = fmaf(dh[i], mi, db[i]);
-                x[i] = dxo[i] + (dh[i] * wb[i] - mi * c1) * rx;          // dx
+                x[i] = dxo[i] + (dh[i] * wb[i] - mi * c1) * rs;          // dx
                 const float dz = a.scale * (GATE ? g[i] : 1.f) * x[i];
                 if (there) da[i] = fmaf(dz, y[i], da[i]);
                 if constexpr (GATE) g[i] = a.scale * x[i] * y[i] * wa[i];                // dgate
@@ -224,7 +265,7 @@ void block_norm_kernel(NormArgs a) {
                     const bool last = row + 1 == end;
                     if (last || n + 1 == a.strip) {                      // the gate's rows in this strip are done
                         if (begin >= first && last) r.store((T*)a.d_gate + (size_t)gate * a.C, dg);
-                        else r.store(a.part + ((size_t)strip * 4 + (begin < first ? 2 : 3)) * a.C, dg);
+                        else r.store(a.gate_part + ((size_t)strip * 2 + (begin < first ? 0 : 1)) * a.C, dg);
 #pragma unroll
                         for (int i = 0; i < EL; ++i) dg[i] = 0.f;
                     }
@@ -232,25 +273,41 @@ void block_norm_kernel(NormArgs a) {
             }
         }
     }
-    if constexpr (BWD) {
-        if (first < a.rows) {
-            if (a.w_after) r.store(a.part + (size_t)strip * 4 * a.C, da);
-            if (a.w_before) r.store(a.part + ((size_t)strip * 4 + 1) * a.C, db);
+    if constexpr (BWD) {                   // the teams' sums of the weights, added in LDS: one row of them a workgroup
+        float* const part = a.part + (size_t)blockIdx.x * 2 * a.C;
+        if constexpr (TEAMS == 1) {
+            if (a.w_after) r.store(part, da);
+            if (a.w_before) r.store(part + a.C, db);
+        } else {
+            __shared__ __attribute__((aligned(16))) float sums[TEAMS][EL * R::TEAM];
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                if (which == 0 ? !a.w_after : !a.w_before) continue;
+                __syncthreads();
+                r.store(sums[team], which == 0 ? da : db);
+                __syncthreads();
+                for (int c = threadIdx.x; c < a.C; c += kThreads(WPR)) {
+                    float sum = sums[0][c];
+#pragma unroll
+                    for (int t = 1; t < TEAMS; ++t) sum += sums[t][c];
+                    part[(size_t)which * a.C + c] = sum;
+                }
+            }
         }
     }
 }
 
-// What strips left, summed: blockIdx.y 0 and 1 the weights (if wanted), from 2 on the gates that no strip holds whole.
-// 32 columns a workgroup, 32 threads a column, each taking every 32nd strip; then in the order of the threads.
+// What workgroups and strips left, summed: blockIdx.y 0 and 1 the weights (if wanted), from 2 on the gates that no strip
+// holds whole.  32 columns a workgroup, 32 threads a column, each taking every 32nd row of sums; then in the threads' order.
 template <class T>
 __global__ __launch_bounds__(1024)
-void block_norm_sum_kernel(const float* __restrict__ part, float* __restrict__ dwa, float* __restrict__ dwb, T* __restrict__ d_gate,
-                           long long rows, long long strip, long long per_gate, int C) {
+void block_norm_sum_kernel(const float* __restrict__ part, const float* __restrict__ gate_part, float* __restrict__ dwa,
+                           float* __restrict__ dwb, T* __restrict__ d_gate, long long rows, long long strip, long long per_gate,
+                           long long wgs, int C) {
     __shared__ float sums[32][33];
     const int cx = threadIdx.x & 31, sy = threadIdx.x >> 5, c = blockIdx.x * 32 + cx;
-    const long long strips = (rows + strip - 1) / strip;
     for (long long which = blockIdx.y; which < 2 + (d_gate ? rows / per_gate : 0); which += gridDim.y) {
-        long long s0 = 0, s1 = strips, begin = 0;
+        long long s0 = 0, s1 = wgs, begin = 0;
         if (which >= 2) {
             begin = (which - 2) * per_gate;
             s0 = begin / strip;
@@ -261,10 +318,9 @@ void block_norm_sum_kernel(const float* __restrict__ part, float* __restrict__ d
         }
         float sum = 0.f;
         if (c < C)
-            for (long long s = s0 + sy; s < s1; s += 32) {
-                const int slot = which < 2 ? (int)which : (begin < s * strip ? 2 : 3);
-                sum += part[((size_t)s * 4 + slot) * C + c];
-            }
+#pragma unroll 4
+            for (long long s = s0 + sy; s < s1; s += 32)
+                sum += which < 2 ? part[((size_t)s * 2 + which) * C + c] : gate_part[((size_t)s * 2 + (begin < s * strip ? 0 : 1)) * C + c];
         sums[sy][cx] = sum;
         __syncthreads();
         if (sy == 0 && c < C) {
@@ -299,19 +355,23 @@ hipError_t launch_c(const NormArgs& a, bool bwd, hipStream_t stream) {
     }
 }
 
-}  // namespace
-
-// Rows of a strip.
-long long block_norm_strip(long long rows, int C, bool bwd) {
-    const int teams = waves_of(C) == 8 ? 1 : 4 / waves_of(C);
-    const long long most = 1024LL * teams;
-    const long long strip = (rows + most - 1) / most;
-    return bwd && strip < 4 ? (rows < 4 ? (rows ? rows : 1) : 4) : (strip ? strip : 1);
+// Rows of a strip, and what the strips leave.  Backward: two workgroups a unit are all that the registers allow, and each
+// leaves a row of sums.
+int teams_of(int C) { return waves_of(C) == 8 ? 1 : 4 / waves_of(C); }
+long long strip_rows(long long rows, int C, bool bwd) {
+    const long long most = (bwd ? (waves_of(C) == 8 ? 256 : 512) : 1024) * teams_of(C), strip = (rows + most - 1) / most;
+    return strip ? strip : 1;
+}
+long long workgroups(long long rows, int C, bool bwd) {
+    const long long strip = strip_rows(rows, C, bwd), strips = (rows + strip - 1) / strip;
+    return (strips + teams_of(C) - 1) / teams_of(C);
 }
 
+}  // namespace
+
 size_t block_norm_part_floats(long long rows, int C) {
-    const long long strip = block_norm_strip(rows, C, true);
-    return (size_t)((rows + strip - 1) / strip) * 4 * C;
+    const long long wgs = workgroups(rows, C, true);
+    return (size_t)wgs * (2 + 2 * teams_of(C)) * C;
 }
 
 hipError_t launch_block_norm(const void* x, const void* y, const void* gate, const float* w_after, const float* w_before,
@@ -342,9 +402,11 @@ hipError_t launch_block_norm(const void* x, const void* y, const void* gate, con
     a.after = after;
     a.C = C;
     a.rows = rows;
-    a.strip = block_norm_strip(rows, C, is_bwd);
+    a.strip = strip_rows(rows, C, is_bwd);
     a.per_gate = gate ? rows / gates : 1;
+    const long long wgs = workgroups(rows, C, true);
     a.part = part;
+    a.gate_part = part ? part + (size_t)wgs * 2 * C : nullptr;
     const int kind = !gate ? kNoGate : (gates == rows ? kElementGate : kSharedGate);
     auto go = [&](auto* t) {
         typedef std::remove_pointer_t<decltype(t)> T;
@@ -359,8 +421,8 @@ hipError_t launch_block_norm(const void* x, const void* y, const void* gate, con
     if (!dwa && !dwb && !shared) return hipSuccess;
     const long long lists = 2 + (shared ? gates : 0);
     const dim3 grid((C + 31) / 32, (unsigned)(lists < 4096 ? lists : 4096));
-    if (is_bf16) hipLaunchKernelGGL(block_norm_sum_kernel<__bf16>, grid, dim3(1024), 0, stream, part, dwa, dwb, shared ? (__bf16*)d_gate : nullptr, rows, a.strip, a.per_gate, C);
-    else hipLaunchKernelGGL(block_norm_sum_kernel<float>, grid, dim3(1024), 0, stream, part, dwa, dwb, shared ? (float*)d_gate : nullptr, rows, a.strip, a.per_gate, C);
+    if (is_bf16) hipLaunchKernelGGL(block_norm_sum_kernel<__bf16>, grid, dim3(1024), 0, stream, a.part, a.gate_part, dwa, dwb, shared ? (__bf16*)d_gate : nullptr, rows, a.strip, a.per_gate, wgs, C);
+    else hipLaunchKernelGGL(block_norm_sum_kernel<float>, grid, dim3(1024), 0, stream, a.part, a.gate_part, dwa, dwb, shared ? (float*)d_gate : nullptr, rows, a.strip, a.per_gate, wgs, C);
     return hipGetLastError();
 }
 

@@ -191,7 +191,6 @@ hipError_t launch_gate(const void* x, const void* u, const void* dy, void* o0, v
 
 // The norms around a block (see ltn_block_norm.hip) on `rows` rows of C features; `gates` rows of gates, each for rows / gates
 // consecutive rows.  is_bwd = 0: o0 = x_out, o1 = h.  is_bwd = 1: o0 = dx, o1 = dy; part: block_norm_part_floats() floats.
-long long block_norm_strip(long long rows, int C, bool bwd);
 size_t block_norm_part_floats(long long rows, int C);
 hipError_t launch_block_norm(const void* x, const void* y, const void* gate, const float* w_after, const float* w_before,
                              const void* d_x_out, const void* d_h, void* o0, void* o1, void* d_gate, float* dwa, float* dwb,
