@@ -713,6 +713,9 @@ def _check_delta(q, k, v, g, beta, cu):
 def ltn_delta_fwd(q, k, v, g, beta, kv_in=None, cu=None, scale=1.0, return_state=False, out=None, kv_out=None):
     """Gated delta rule: S_t = exp(g_t) S_{t-1} corrected by beta_t k_t (v_t - ..)^T, o_t = scale S_t^T q_t, optionally continuing
     from / returning the fp32 states [rows,H,Dk,Dv].  cu: ends of packed sequences (int32, on the GPU, Bt = 1)."""
+    r = _fast().delta_fwd(q, k, v, g, beta, kv_in, cu, scale, return_state, out, kv_out)
+    if r is not None:
+        return r
     lib = load_library()
     Bt, Hk, H, N, Dk, Dv, seqs, rows = _check_delta(q, k, v, g, beta, cu)
     o = torch.empty_like(v) if out is None else _out(out, "out", v.numel(), v.dtype)
@@ -736,6 +739,10 @@ def ltn_delta_fwd(q, k, v, g, beta, kv_in=None, cu=None, scale=1.0, return_state
 
 def ltn_delta_bwd(q, k, v, g, beta, d_o, cu=None, scale=1.0, out=None):
     """(dq, dk, dv, dg, dbeta) of ltn_delta_fwd from zero initial states, all in q's dtype."""
+    if out is None:
+        r = _fast().delta_bwd(q, k, v, g, beta, d_o, cu, scale)
+        if r is not None:
+            return r
     lib = load_library()
     Bt, Hk, H, N, Dk, Dv, seqs, _ = _check_delta(q, k, v, g, beta, cu)
     _dev(d_o, "d_o")
@@ -758,6 +765,9 @@ def ltn_delta_bwd(q, k, v, g, beta, d_o, cu=None, scale=1.0, out=None):
 
 def ltn_delta_decode_steps(q, k, v, kv, g, beta, scale=1.0, out=None):
     """S steps of the gated delta rule: q, k [Bt,Hk,S,Dk]; v [Bt,H,S,Dv]; kv fp32 [Bt,H,Dk,Dv] updated in place; returns o."""
+    r = _fast().delta_decode_steps(q, k, v, kv, g, beta, scale, out)
+    if r is not None:
+        return r
     lib = load_library()
     Bt, Hk, H, S, Dk, Dv, _, _ = _check_delta(q, k, v, g, beta, None)
     _dev(kv, "kv")
@@ -807,6 +817,10 @@ def _check_block_norm(x, y, gate, w_after, w_before, after, others=()):
 def ltn_block_norm_fwd(x, y, gate=None, w_after=None, w_before=None, scale=1.0, eps=0.0, after=True, out=None):
     """(x_out, h): x_out = x + scale gate (.) norm(y) (.) w_after, h = norm(x_out) (.) w_before over the last axis, with
     norm(t) = t / sqrt(mean(t^2) + eps) (after=False: y itself).  gate: [.., C] whose rows each serve as many of x's."""
+    if out is None:
+        r = _fast().block_norm_fwd(x, y, gate, w_after, w_before, scale, eps, after)
+        if r is not None:
+            return r
     lib = load_library()
     rows, gates, C = _check_block_norm(x, y, gate, w_after, w_before, after)
     if out is None:
@@ -823,6 +837,9 @@ def ltn_block_norm_fwd(x, y, gate=None, w_after=None, w_before=None, scale=1.0, 
 def ltn_block_norm_bwd(x, y, d_x_out, d_h, gate=None, w_after=None, w_before=None, scale=1.0, eps=0.0, after=True):
     """(d_x, d_y, d_gate, d_w_after, d_w_before) of ltn_block_norm_fwd from its inputs; None in the place of what it had none
     of.  d_x_out: the gradient by x_out, or None (zero)."""
+    r = _fast().block_norm_bwd(x, y, d_x_out, d_h, gate, w_after, w_before, scale, eps, after)
+    if r is not None:
+        return r
     lib = load_library()
     others = [("d_h", d_h)] + ([] if d_x_out is None else [("d_x_out", d_x_out)])
     rows, gates, C = _check_block_norm(x, y, gate, w_after, w_before, after, others)

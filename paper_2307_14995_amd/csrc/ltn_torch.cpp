@@ -29,7 +29,10 @@ namespace {
     X(fwd_dkdv, ltn_attn_fwd_dkdv) X(bwd_dkdv, ltn_attn_bwd_dkdv)                                                \
     X(decode_steps_dkdv, ltn_attn_decode_steps_dkdv) X(workspace_bytes_dkdv, ltn_attn_workspace_bytes_dkdv)      \
     X(prologue_fwd, ltn_prologue_fwd) X(prologue_bwd, ltn_prologue_bwd)                                          \
-    X(prologue_workspace_bytes, ltn_prologue_workspace_bytes)
+    X(prologue_workspace_bytes, ltn_prologue_workspace_bytes)                                                    \
+    X(delta_fwd, ltn_delta_fwd) X(delta_bwd, ltn_delta_bwd) X(delta_decode_steps, ltn_delta_decode_steps)        \
+    X(delta_workspace_bytes, ltn_delta_workspace_bytes) X(block_norm_fwd, ltn_block_norm_fwd)                    \
+    X(block_norm_bwd, ltn_block_norm_bwd) X(block_norm_workspace_bytes, ltn_block_norm_workspace_bytes)
 struct Library {
 #define LTN_FIELD(field, symbol) decltype(&symbol) field;
     LTN_LIBRARY(LTN_FIELD)
@@ -451,6 +454,170 @@ PyObject* prologue_bwd(const Args& x) {
     return tuple(r);
 }
 
+// Queries and keys of Hk heads, values of H, gates of a value head and token; packed sequences by their ends.
+struct Delta : Dims {
+    int Hk, Dv, seqs = 0, rows;            // (Dims::H: that of the values, rows: states)
+    ltn_dtype dt;
+    const float *g, *beta;
+    const int* cu = nullptr;
+    Delta(const Args& x, int gi, int bi, int cui) : Dims(x.tensor(2)) {
+        const at::Tensor &q = x.tensor(0), &k = x.tensor(1), &v = x.tensor(2), &gt = x.tensor(gi), &bt = x.tensor(bi);
+        same(q, k);
+        need(q.dim() == 4 && q.scalar_type() == v.scalar_type() && q.size(0) == v.size(0) && q.size(2) == v.size(2) &&
+             q.size(1) <= INT32_MAX && q.size(3) <= INT32_MAX);
+        Dv = D;
+        D = (int)q.size(3);
+        Hk = (int)q.size(1);
+        need(H == 0 || (Hk > 0 && H % Hk == 0));
+        for (const at::Tensor* t : {&gt, &bt})
+            need(t->scalar_type() == at::kFloat && t->sizes() == at::IntArrayRef({Bt, H, N}));
+        g = (const float*)gt.data_ptr();
+        beta = (const float*)bt.data_ptr();
+        dt = dtype_of(q);
+        rows = Bt;
+        if (cui >= 0 && !x.none(cui)) {
+            const at::Tensor& c = x.tensor(cui);
+            need(c.scalar_type() == at::kInt && c.dim() == 1 && c.numel() >= 2 && c.numel() <= INT32_MAX && Bt == 1);
+            seqs = rows = (int)c.numel() - 1;
+            cu = (const int*)c.data_ptr();
+        }
+    }
+};
+
+// q, k, v, g, beta, kv_in, cu, scale, return_state, out, kv_out
+PyObject* delta_fwd(const Args& x) {
+    const at::Tensor &q = x.tensor(0), &k = x.tensor(1), &v = x.tensor(2);
+    const Delta d(x, 3, 4, 6);
+    const std::array<int64_t, 4> state = {d.rows, d.H, d.D, d.Dv};
+    const float* kv_in = x.state(5, state);
+    const float scale = x.real(7);
+    const bool want = x.flag(8);
+    const Out o(x, 9, v);
+    Out kv;
+    kv.state(x, 10, want, state, q);
+    const size_t n = lib.delta_workspace_bytes(d.Bt, d.H, d.N, d.D, d.Dv, d.seqs, d.dt, 0);
+    const at::Tensor ws = scratch(n, q);
+    call("ltn_delta_fwd", [&] {
+        return lib.delta_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.ptr, d.g, d.beta, d.cu, kv_in, (float*)kv.ptr, scale,
+                             d.Bt, d.Hk, d.H, d.N, d.D, d.Dv, d.seqs, d.dt, at_or_null(ws), n, x.stream());
+    });
+    if (!want && x.none(10)) return o.object();
+    const Out* r[] = {&o, &kv};
+    return tuple(r);
+}
+
+// q, k, v, g, beta, d_o, cu, scale (the gradients are allocated here)
+PyObject* delta_bwd(const Args& x) {
+    const at::Tensor &q = x.tensor(0), &k = x.tensor(1), &v = x.tensor(2), &go = x.tensor(5);
+    const Delta d(x, 3, 4, 6);
+    same(v, go);
+    const float scale = x.real(7);
+    Out dq, dk, dv, dg, db;
+    dq.make(at::empty_like(q));
+    dk.make(at::empty_like(k));
+    dv.make(at::empty_like(v));
+    for (Out* o : {&dg, &db}) o->make(at::empty({d.Bt, d.H, d.N}, q.options()));
+    const size_t n = lib.delta_workspace_bytes(d.Bt, d.H, d.N, d.D, d.Dv, d.seqs, d.dt, 1);
+    const at::Tensor ws = scratch(n, q);
+    call("ltn_delta_bwd", [&] {
+        return lib.delta_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), go.data_ptr(), dq.ptr, dk.ptr, dv.ptr, dg.ptr, db.ptr, d.g,
+                             d.beta, d.cu, scale, d.Bt, d.Hk, d.H, d.N, d.D, d.Dv, d.seqs, d.dt, at_or_null(ws), n, x.stream());
+    });
+    const Out* r[] = {&dq, &dk, &dv, &dg, &db};
+    return tuple(r);
+}
+
+// q, k, v, kv, g, beta, scale, out
+PyObject* delta_decode_steps(const Args& x) {
+    const at::Tensor &q = x.tensor(0), &k = x.tensor(1), &v = x.tensor(2), &kv = x.tensor(3);
+    const Delta d(x, 4, 5, -1);
+    need(d.N <= INT32_MAX && kv.scalar_type() == at::kFloat && kv.sizes() == at::IntArrayRef({d.Bt, d.H, d.D, d.Dv}));
+    const float scale = x.real(6);
+    const Out o(x, 7, v);
+    call("ltn_delta_decode_steps", [&] {
+        return lib.delta_decode_steps(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.ptr, (float*)kv.data_ptr(), d.g, d.beta, scale,
+                                      d.Bt, d.Hk, d.H, (int)d.N, d.D, d.Dv, d.dt, x.stream());
+    });
+    return o.object();
+}
+
+// Rows of C features with a gate and weights, any of them none.
+struct Rows {
+    long long rows, gates = 0;
+    int C;
+    ltn_dtype dt;
+    const void* gate = nullptr;
+    const float *w_after, *w_before;
+    Rows(const Args& x, int gi, int ai, int bi) {
+        const at::Tensor& t = x.tensor(0);
+        need(t.dim() >= 1 && t.numel() > 0 && t.size(-1) <= INT32_MAX);
+        C = (int)t.size(-1);
+        rows = t.numel() / C;
+        dt = dtype_of(t);
+        if (!x.none(gi)) {
+            const at::Tensor& g = x.tensor(gi);
+            need(g.scalar_type() == t.scalar_type() && g.dim() >= 1 && g.size(-1) == C && g.numel() > 0);
+            gates = g.numel() / C;
+            need(rows % gates == 0);
+            gate = g.data_ptr();
+        }
+        w_after = weight(x, ai);
+        w_before = weight(x, bi);
+    }
+    const float* weight(const Args& x, int i) const {
+        if (x.none(i)) return nullptr;
+        const at::Tensor& w = x.tensor(i);
+        need(w.scalar_type() == at::kFloat && w.sizes() == at::IntArrayRef({C}));
+        return (const float*)w.data_ptr();
+    }
+};
+
+// x, y, gate, w_after, w_before, scale, eps, after (the outputs are allocated here)
+PyObject* block_norm_fwd(const Args& x) {
+    const at::Tensor &t = x.tensor(0), &y = x.tensor(1);
+    same(t, y);
+    const Rows d(x, 2, 3, 4);
+    const float scale = x.real(5), eps = x.real(6);
+    const bool after = x.flag(7);
+    Out xo, h;
+    for (Out* o : {&xo, &h}) o->make(at::empty_like(t));
+    call("ltn_block_norm_fwd", [&] {
+        return lib.block_norm_fwd(t.data_ptr(), y.data_ptr(), d.gate, d.w_after, d.w_before, xo.ptr, h.ptr, scale, eps, after, d.rows,
+                                  d.gates, d.C, d.dt, x.stream());
+    });
+    const Out* r[] = {&xo, &h};
+    return tuple(r);
+}
+
+// x, y, d_x_out, d_h, gate, w_after, w_before, scale, eps, after
+PyObject* block_norm_bwd(const Args& x) {
+    const at::Tensor &t = x.tensor(0), &y = x.tensor(1), &dh = x.tensor(3);
+    same(t, y);
+    same(t, dh);
+    const void* dxo = nullptr;
+    if (!x.none(2)) {
+        same(t, x.tensor(2));
+        dxo = x.tensor(2).data_ptr();
+    }
+    const Rows d(x, 4, 5, 6);
+    const float scale = x.real(7), eps = x.real(8);
+    const bool after = x.flag(9);
+    Out dx, dy, dgate, dwa, dwb;
+    for (Out* o : {&dx, &dy}) o->make(at::empty_like(t));
+    if (d.gate) dgate.make(at::empty_like(x.tensor(4)));
+    if (d.w_after) dwa.make(at::empty_like(x.tensor(5)));
+    if (d.w_before) dwb.make(at::empty_like(x.tensor(6)));
+    const size_t n = lib.block_norm_workspace_bytes(d.rows, d.C);
+    const at::Tensor ws = scratch(n, t);
+    call("ltn_block_norm_bwd", [&] {
+        return lib.block_norm_bwd(t.data_ptr(), y.data_ptr(), d.gate, d.w_after, d.w_before, dxo, dh.data_ptr(), dx.ptr, dy.ptr,
+                                  dgate.ptr, (float*)dwa.ptr, (float*)dwb.ptr, scale, eps, after, d.rows, d.gates, d.C, d.dt,
+                                  at_or_null(ws), n, x.stream());
+    });
+    const Out* r[] = {&dx, &dy, d.gate ? &dgate : nullptr, d.w_after ? &dwa : nullptr, d.w_before ? &dwb : nullptr};
+    return tuple(r);
+}
+
 template <PyObject* (*F)(const Args&), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -496,7 +663,9 @@ PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
     LTN_ENTRY(fwd, 9), LTN_ENTRY(fwd_gated, 13), LTN_ENTRY(bwd, 6), LTN_ENTRY(gate_bwd, 4), LTN_ENTRY(decode_step, 6),
     LTN_ENTRY(decode_steps, 6), LTN_ENTRY(fwd_dkdv, 9), LTN_ENTRY(bwd_dkdv, 6), LTN_ENTRY(decode_steps_dkdv, 6),
-    LTN_ENTRY(prologue_fwd, 5), LTN_ENTRY(prologue_bwd, 6), {nullptr, nullptr, 0, nullptr}};
+    LTN_ENTRY(prologue_fwd, 5), LTN_ENTRY(prologue_bwd, 6),
+    LTN_ENTRY(delta_fwd, 11), LTN_ENTRY(delta_bwd, 8), LTN_ENTRY(delta_decode_steps, 8), LTN_ENTRY(block_norm_fwd, 8),
+    LTN_ENTRY(block_norm_bwd, 10), {nullptr, nullptr, 0, nullptr}};
 #undef LTN_ENTRY
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ltn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
