@@ -39,12 +39,17 @@ template <class T> struct Turn {
         lds_write(in + b * 128, f.a);
         lds_write(in + b * 128 + 16, f.b);
     }
-    __device__ __forceinline__ void store(__bf16* p, int rt) const { *(s16x4*)p = lds_read_tr(out ^ (rt << 5)); }
-    __device__ __forceinline__ void store(float* p, int rt) const {
+    // (the transposing read takes part of every lane's row: all lanes make it, also those whose token is past the end)
+    __device__ __forceinline__ void store(__bf16* p, int rt, bool there) const {
+        s16x4 x = lds_read_tr(out ^ (rt << 5));
+        asm volatile("" : "+v"(x));
+        if (there) *(s16x4*)p = x;
+    }
+    __device__ __forceinline__ void store(float* p, int rt, bool there) const {
         f32x4 x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = lds_read<float>(out + 64 * rt + i * Ti::RB);
-        *(f32x4*)p = x;
+        if (there) *(f32x4*)p = x;
     }
 };
 
@@ -478,14 +483,10 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], xf[b], S[t][c]);
             T* const out = (T*)a.dv + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
-            if (rows == kChunk) {
+            // (of one wave, and in order: no wait but the reads' own)
+            asm volatile("" ::: "memory");
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) turn.store(out + (size_t)(16 * rt) * Dv, rt);
-            } else {
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt)
-                    if (16 * rt + m < rows) turn.store(out + (size_t)(16 * rt) * Dv, rt);
-            }
+            for (int rt = 0; rt < 4; ++rt) turn.store(out + (size_t)(16 * rt) * Dv, rt, 16 * rt + m < rows);
         }
         if constexpr (BF) {
             const int by = chunk & 1 ? -L::BYTES : L::BYTES;
