@@ -72,8 +72,9 @@ inline DeltaScratch delta_scratch(int Dk, int Dv, bool bf16) {
 }
 inline size_t delta_bytes(int Dk, int Dv, bool bf16, bool bwd) {
     const DeltaScratch s = delta_scratch(Dk, Dv, bf16);
-    // T' (bf16: in two parts), P and decays; for the gradients Z, the states before chunks and their derivatives behind them
-    return (2 + (bf16 ? 1 : 0)) * s.tile + s.vec + (bwd ? s.z + 2 * s.state : 0);
+    // T' (bf16: in two parts, for the fp32 state handed out; the gradients take the first), P and decays; for the gradients
+    // Z, the states before chunks and their derivatives behind them
+    return (bf16 && !bwd ? 3 : 2) * s.tile + s.vec + (bwd ? s.z + 2 * s.state : 0);
 }
 
 hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream);

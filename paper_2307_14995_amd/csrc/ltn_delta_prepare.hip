@@ -192,7 +192,8 @@ void delta_prepare_kernel(DeltaArgs a) {
         }
         const F f = frag_of<T>(x, y);
         *(F*)((T*)(a.tq + at * kTile) + n * kChunk + c) = f;
-        if constexpr (sizeof(T) == 2) *(F*)((T*)(a.tl + at * kTile) + n * kChunk + c) = rest_of(f, x, y);
+        if constexpr (sizeof(T) == 2)
+            if (a.tl) *(F*)((T*)(a.tl + at * kTile) + n * kChunk + c) = rest_of(f, x, y);
     }
 }
 

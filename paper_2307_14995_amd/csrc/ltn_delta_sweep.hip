@@ -60,10 +60,10 @@ template <class T> __device__ __forceinline__ void fence() {
     if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
 }
 
-// One chunk's tiles in LDS.  FWD: K, T', its second part (bf16), V and, where O is wanted, Q and P.  Backward: K, Q, T', P, dO.
+// One chunk's tiles in LDS.  FWD: K, T', V and, where O is wanted, T's second part (bf16), Q and P.  Backward: K, Q, T', P, dO.
 template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
-                         T2 = VEC + 1024, Q = T2 + (FWD && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
+                         T2 = VEC + 1024, Q = T2 + (FWD && FULL && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
                          P = Q + (FULL ? Tile<T, DK>::BYTES : 0), BYTES = P + (FULL ? Tile<T, kChunk>::BYTES : 0);
     static constexpr int BUFS = sizeof(T) == 2 ? 2 : 1, ALL = BUFS * BYTES;                   // of a workgroup
     static_assert(ALL <= 160 * 1024, "LDS");
@@ -89,7 +89,7 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
         k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::K, w, lane);
         t1.fetch(a.tq + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T1, w, lane);
         v.fetch((const char*)(FWD ? a.v : a.d_o) + (val_row * Dv + col0) * sizeof(T), Dv * sizeof(T), rows, lds + L::V, w, lane);
-        if constexpr (FWD && BF) t2.fetch(a.tl + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T2, w, lane);
+        if constexpr (FWD && FULL && BF) t2.fetch(a.tl + at * kTile, kChunk * sizeof(T), kChunk, lds + L::T2, w, lane);
         if constexpr (FULL) {
             q.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, lds + L::Q, w, lane);
             p.fetch(a.p + at * kTile, kChunk * sizeof(T), kChunk, lds + L::P, w, lane);
@@ -186,7 +186,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             const int col = c0 + 16 * c;
             const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
             F rd[4 * (NT / 2)];            // K's rows, then Q's, then K's columns
-            F tf[6], tl[BF ? 6 : 1], pf[6];        // T' in two parts, P: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
+            F tf[6], tl[BF ? 6 : 1], pf[6];        // T' (in two parts where O is wanted), P: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
             f32x4 V[4], gam[4], bt[4], en[4], Z[4], O[4];
             float row_gam[4];
             auto k_cols = [&](int i) { return k_col.frag(L::K, i / NT, i % NT); };
@@ -224,7 +224,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
                 }
                 fence<T>();
             }
-            if constexpr (BF)
+            if constexpr (BF && !SAVE)
 #pragma unroll
                 for (int i = 0; i < 6; ++i) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
             fence<T>();
@@ -251,8 +251,9 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             if constexpr (BF) {
 #pragma unroll
                 for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xl[i / 4], Z[i < 4 ? i : i - 2]);
+                if constexpr (!SAVE)
 #pragma unroll
-                for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
+                    for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
             }
             fence<T>();
             // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory

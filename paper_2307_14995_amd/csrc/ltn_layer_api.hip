@@ -48,7 +48,7 @@ size_t lay_out(ltn::DeltaArgs& a, char* base, int Dk, int Dv, bool bf16, bool bw
         return at;
     };
     a.tq = take(s.tile);
-    if (bf16) a.tl = take(s.tile);
+    if (bf16 && !bwd) a.tl = take(s.tile);
     a.p = take(s.tile);
     a.vec = reinterpret_cast<float*>(take(s.vec));
     if (bwd) {
