@@ -206,12 +206,16 @@ __device__ __forceinline__ unsigned hide(unsigned x) {
     return x;
 }
 
+// A reader's address 32 kb columns on, kb a multiple of the power of two that the columns it then reads are fewer than.
+template <class T> __device__ __forceinline__ unsigned skip_columns(unsigned at, int kb) { return sizeof(T) == 2 ? at ^ (kb << 6) : at + kb * 128; }
+
 // Eight elements of one row, from column 32 kb + 8 (lane / 16) on.
 template <class T, int COLS> struct RowReader {
     unsigned b;
     __device__ __forceinline__ RowReader(unsigned lds, int row, int lane)
         : b(lds + Tile<T, COLS>::chunk(row, (sizeof(T) == 2 ? 1 : 2) * (lane >> 4))) {}
     __device__ __forceinline__ void move(int by) { b += by; }
+    __device__ __forceinline__ void skip(int kb) { b = skip_columns<T>(b, kb); }
     __device__ __forceinline__ typename El<T>::F frag(int tile, int kb) const {
         return lds_frag<T>(sizeof(T) == 2 ? (b ^ (kb << 6)) + tile : b + tile + kb * 128);
     }
@@ -224,6 +228,10 @@ template <class T, int COLS> struct PairedRowReader {
     __device__ __forceinline__ void move(int by) {
         even += by;
         odd += by;
+    }
+    __device__ __forceinline__ void skip(int kb) {
+        even = skip_columns<T>(even, kb);
+        odd = skip_columns<T>(odd, kb);
     }
     __device__ __forceinline__ typename El<T>::F frag(int tile, int rt, int kb) const {
         RowReader<T, COLS> r = {0, 0, 0};
@@ -247,6 +255,10 @@ template <class T, int COLS, bool PAIRED> struct ColReader {
     __device__ __forceinline__ void move(int by) {                       // by a multiple of 1 KB
         lo += by;
         hi += by;
+    }
+    __device__ __forceinline__ void skip(int kb) {
+        lo = skip_columns<T>(lo, kb);
+        hi = skip_columns<T>(hi, kb);
     }
     __device__ __forceinline__ void hide_all() {
         lo = hide(lo);

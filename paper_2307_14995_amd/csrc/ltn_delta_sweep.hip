@@ -1,15 +1,27 @@
-// Gated delta rule: the sweeps over the chunks of a chain (ltn_delta.h has the formulas).  A wave owns 16 CT columns of the
+// Gated delta rule: the sweeps over the chunks of a chain (ltn_delta.h has the formulas).  A wave owns 16 columns of the
 // state: all Dk rows of them stay in its accumulators from the first chunk to the last, and as the columns of S, X, Z, U,
-// O (and of dS, dU, dY) are independent, no wave ever waits for another's result.  The state's rows and the tokens are dealt
+// O (and of dS, dU, dV) are independent, no wave waits for another's result.  The state's rows and the tokens are dealt
 // to the accumulators' rows so (paired()) that one product's results are, lane by lane, the next one's right operand:
-// nothing between the products passes through LDS.  What the waves share are the chunk's tiles, the left operands.
+// nothing between the products passes through LDS.  What the four waves share are the chunk's tiles, the left operands.
 //
-// bf16: the tiles of the next chunk are fetched into a second buffer by a wave that does nothing else.  (The waves that
-// compute spent two thirds of a chunk's 3.7 us on issuing those loads: a wave's next load waits until the memory path has taken the last one.)
+// bf16: the tiles of the next chunk are fetched into a second buffer by four waves that do nothing else.  (A wave's next
+// load waits until the memory path has taken its last one, 57 to 90 cycles; the waves that compute spent two thirds of a
+// chunk's 3.7 us on issuing those loads, and one fetching wave still took longer than a chunk.)  The tiles of two chunks
+// and some 250 registers a wave make it one workgroup a compute unit.
 //
-// bf16: S, X, U and T' enter the products of the state in two parts of 8 bits of significand each (three products of
-// four for T' X): the state that the forward hands on is fp32 and stays as exact as sums of fp32 products to some 4e-6;
-// in one part each it would be off by 2.4e-3.  O, rounded to bf16 anyway, takes the larger parts alone.
+// bf16: S, X, U and, where O is wanted, T' enter the products of the state in two parts of 8 bits of significand each
+// (three products of four for T' X): the state that the forward hands on is fp32 and stays as exact as sums of fp32
+// products to some 4e-6; in one part each it would be off by 2.4e-3.  O, rounded to bf16 anyway, takes the larger parts
+// alone, and so do the gradients, but for the state that they carry along.
+//
+// fp32 (matrix products at a sixteenth of the bf16 rate, which bound it): while there are workgroups for no more than
+// half of the compute units, two waves share 16 columns, each with half of the features, and add their parts of K S and
+// Q S through LDS.  Two rows of 700 tokens, 8 heads of 64: forward 75 -> 60 us, the gradients' sweeps 53 -> 40 and 84 ->
+// 67.  (bf16 gains nothing from it: one prompt of 3001 tokens 116 us either way.)
+//
+// What bounds them, heads of 128 features: 256 or more workgroups, HBM (4 rows of 8192 tokens, 32 heads, bf16: forward 326
+// us at 4.4 TB/s, the gradients' two 312 and 425); fewer, a chunk's chain of dependent steps, 1.9 to 2.4 us, in which LDS
+// serves 340 KB of operands (3100 of 4700 cycles; matrix products take 1700): one prompt of 3001 tokens, 47 chunks, 96 us.
 #include "ltn_delta.h"
 
 namespace ltn {
@@ -29,10 +41,10 @@ template <class T> struct Turn {
     typedef Tile<T, kChunk> Ti;
     static constexpr int BYTES = 16 * Ti::RB;
     unsigned in, out;
-    __device__ __forceinline__ Turn(unsigned lds, int lane) {
+    __device__ __forceinline__ Turn(unsigned lds, int lane, int first) {     // store() numbers row tiles from `first` on
         const int m = lane & 15, grp = lane >> 4;
         in = lds + Ti::chunk(m, sizeof(T) == 2 ? grp : 2 * grp);
-        out = lds + (sizeof(T) == 2 ? Ti::at(4 * grp + (m >> 2), 4 * (m & 3)) : Ti::at(4 * grp, m));
+        out = sizeof(T) == 2 ? (lds + Ti::at(4 * grp + (m >> 2), 4 * (m & 3))) ^ (first << 5) : lds + Ti::at(4 * grp, m + 16 * first);
     }
     __device__ __forceinline__ void write(int b, const bf16x8& f) const { lds_write(in ^ (b << 6), f); }
     __device__ __forceinline__ void write(int b, const F32Frag& f) const {
@@ -60,6 +72,9 @@ template <class T> __device__ __forceinline__ void fence() {
     if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
 }
 
+// What a wave hands the one that has the other features of its columns: K S (or K dS), and O's other two row tiles.
+template <bool SAVE> struct Swap { static constexpr int BYTES = (SAVE ? 4 : 6) * 1024; };
+
 // One chunk's tiles in LDS.  FWD: K, T', V and, where O is wanted, T's second part (bf16), Q and P.  Backward: K, Q, T', P, dO.
 template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
@@ -69,13 +84,13 @@ template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static_assert(ALL <= 160 * 1024, "LDS");
 };
 
-// Waves that fetch: one besides those that compute (bf16), or all of these (fp32, through registers).
-constexpr int kFetchers = 4;
-template <class T> constexpr int fetchers(int W) { return sizeof(T) == 2 ? kFetchers : W; }
-template <class T> constexpr int threads_of(int W) { return 64 * (sizeof(T) == 2 ? W + kFetchers : W); }
+// Waves that compute, and waves that fetch besides them (bf16; fp32: the same, through registers).
+constexpr int W = 4, kFetchers = 4;
+static_assert(W == kFetchers, "either kind of waves fetches alike");
+template <class T> constexpr int kThreadsOf = 64 * (sizeof(T) == 2 ? W + kFetchers : W);
 
-// The fetches of a chunk's tiles by W waves.
-template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFetch {
+// The fetches of a chunk's tiles.
+template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepFetch {
     typedef SweepLds<T, DK, COLS, FULL, FWD> L;
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr size_t kTile = (size_t)kChunk * kChunk * sizeof(T);
@@ -115,11 +130,12 @@ template <class T, int DK, int COLS, int W, bool FULL, bool FWD> struct SweepFet
 };
 
 // Forward.  SAVE: Z and the states before chunks are written, for the gradients, and O is not.
-template <class T, int DK, int CT, int W, bool SAVE>
-__global__ __launch_bounds__(threads_of<T>(W)) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+template <class T, int DK, int KS, bool SAVE>
+__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int COLS = 16 * CT * W, NT = DK / 16;
+    static_assert(KS == 1 || !BF, "the waves that fetch take no part in the exchange");
+    constexpr int COLS = 16 * W / KS, NT = DK / 16 / KS, NP = NT / 2, NO = 4 / KS;
     typedef typename El<T>::F F;
     typedef SweepLds<T, DK, COLS, !SAVE, true> L;
     extern __shared__ __attribute__((aligned(1024))) char lds[];        // (of a size unknown to the compiler, which would else plan for one wave a SIMD and move accumulators to and fro)
@@ -130,12 +146,12 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
     const unsigned lds0 = lds_address(lds);
-    const int wg0 = split * COLS, c0 = 16 * CT * w;                      // the workgroup's and the wave's first column
+    const int wg0 = split * COLS, c0 = 16 * (w / KS), part = w % KS, f0 = part * (DK / KS);    // the workgroup's and the wave's first column, the wave's first feature
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
 
     const int chunks = (s.len + kChunk - 1) / kChunk;
-    SweepFetch<T, DK, COLS, fetchers<T>(W), !SAVE, true> next;
+    SweepFetch<T, DK, COLS, !SAVE, true> next;
     auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
@@ -150,28 +166,32 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         }
         return;
     }
-    f32x4 S[NT][CT];
+    f32x4 S[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) S[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) S[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (a.kv_in) {
-        const float* in = a.kv_in + (size_t)chain * DK * Dv + wg0 + c0 + m;
+        const float* in = a.kv_in + ((size_t)chain * DK + f0) * Dv + wg0 + c0 + m;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[t][c][i] = in[(size_t)(token_of(t, grp) + i) * Dv + 16 * c];   // (features are dealt as tokens)
+            for (int i = 0; i < 4; ++i) S[t][i] = in[(size_t)(token_of(t, grp) + i) * Dv];   // (features are dealt as tokens)
     }
     if (!BF && chunks) fetch(0);
     PairedRowReader<T, DK> k_row(lds0, lane);
     ColReader<T, DK, true> k_col(lds0, lane);
     PairedRowReader<T, kChunk> t_row(lds0, lane);
     ColReader<T, COLS, false> v_col(lds0, lane);
-    RowReader<T, DK> q_row(lds0, m, lane);
-    RowReader<T, kChunk> p_row(lds0, m, lane);
     constexpr int RD = Tile<T, DK>::RB, RC = Tile<T, kChunk>::RB;
+    // Of O a wave ends with row tiles part, part + KS, ..: Q's rows for these and for the others', P's for these
+    RowReader<T, DK> q_row(lds0 + 16 * RD * part, m, lane), q_others(lds0 + 16 * RD * (KS - 1 - part), m, lane);
+    RowReader<T, kChunk> p_row(lds0 + 16 * RC * part, m, lane);
+    if constexpr (KS > 1) {
+        k_row.skip(NP * part);
+        k_col.skip(NP * part);
+        q_row.skip(NP * part);
+        q_others.skip(NP * part);
+    }
+    const unsigned mine = lds0 + L::ALL + w * Swap<SAVE>::BYTES + lane * 16, others = lds0 + L::ALL + (w ^ 1) * Swap<SAVE>::BYTES + lane * 16;
     unsigned vec = lds0 + L::VEC;          // gam, end, beta
     auto vec4 = [&](int which, int rt) { return lds_read<f32x4>(vec + 32 * grp + 4 * (which * kChunk + token_of(rt, 0))); };
     for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -181,137 +201,151 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         __syncthreads();
         if (!BF && chunk + 1 < chunks) fetch(chunk + 1);
 
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        F rd[4 * (NP)];            // K's rows, then Q's, then K's columns
+        F tf[6], tl[BF ? 6 : 1], pf[6];        // T' (in two parts where O is wanted), P: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
+        f32x4 V[4], gam[4], bt[4], en[4], Z[4], O[4];
+        float row_gam[4];
+        auto k_cols = [&](int i) { return k_col.frag(L::K, i / NT, i % NT); };
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const int col = c0 + 16 * c;
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            F rd[4 * (NT / 2)];            // K's rows, then Q's, then K's columns
-            F tf[6], tl[BF ? 6 : 1], pf[6];        // T' (in two parts where O is wanted), P: row tiles 0 .. 3 of the first 32 columns, 2, 3 of the second
-            f32x4 V[4], gam[4], bt[4], en[4], Z[4], O[4];
-            float row_gam[4];
-            auto k_cols = [&](int i) { return k_col.frag(L::K, i / NT, i % NT); };
+        for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
+        const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
 #pragma unroll
-            for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
-            const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
+        for (int rt = 0; rt < 4; ++rt) {
+            V[rt] = v_col.values(L::V, rt, c0 / 16);
+            gam[rt] = vec4(0, rt);
+        }
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                V[rt] = v_col.values(L::V, rt, col / 16);
-                gam[rt] = vec4(0, rt);
-            }
+        for (int i = 0; i < 6; ++i) tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
+        fence<T>();
+        F Sh[NP], Sl[BF ? NP : 1];
 #pragma unroll
-            for (int i = 0; i < 6; ++i) tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
-            fence<T>();
-            F Sh[NT / 2], Sl[BF ? NT / 2 : 1];
+        for (int p = 0; p < NP; ++p) {
+            Sh[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
+            if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p], S[2 * p + 1]);
+            if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sh[p]);
+        }
+        fence<T>();
 #pragma unroll
-            for (int p = 0; p < NT / 2; ++p) {
-                Sh[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
-                if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p][c], S[2 * p + 1][c]);
-                if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sh[p]);
-            }
-            fence<T>();
+        for (int p = 0; p < NP; ++p) {
 #pragma unroll
-            for (int p = 0; p < NT / 2; ++p) {
+            for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sh[p], p ? Z[rt] : zero);
+            if constexpr (BF)
 #pragma unroll
-                for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sh[p], p ? Z[rt] : zero);
-                if constexpr (BF)
-#pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sl[p], Z[rt]);
-                fence<T>();
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) {
-                    if constexpr (SAVE) rd[4 * p + rt] = k_cols(4 * p + rt);
-                    else rd[4 * p + rt] = q_row.frag(L::Q + 16 * rt * RD, p);
-                }
-                fence<T>();
-            }
-            if constexpr (BF && !SAVE)
-#pragma unroll
-                for (int i = 0; i < 6; ++i) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] = V[rt] - gam[rt] * Z[rt];
-            F Xh[2], Xl[BF ? 2 : 1];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                Xh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
-                if constexpr (BF) Xl[b] = rest_of(Xh[b], Z[2 * b], Z[2 * b + 1]);
-            }
+                for (int rt = 0; rt < 4; ++rt) Z[rt] = mma(rd[4 * p + rt], Sl[p], Z[rt]);
             fence<T>();
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
-                bt[rt] = vec4(2, rt);
-                en[rt] = vec4(1, rt);
-                if constexpr (!SAVE) row_gam[rt] = lds_read<float>(vec + 4 * m + 64 * rt) * a.scale;
+                if constexpr (SAVE) rd[4 * p + rt] = k_cols(4 * p + rt);
+                else rd[4 * p + rt] = (rt < NO ? q_row : q_others).frag(L::Q + 16 * KS * (rt % NO) * RD, p);
             }
             fence<T>();
+        }
+        auto q_state = [&] {
 #pragma unroll
-            for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
-            if constexpr (BF) {
+            for (int p = 0; p < NP; ++p) {
 #pragma unroll
-                for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xl[i / 4], Z[i < 4 ? i : i - 2]);
-                if constexpr (!SAVE)
-#pragma unroll
-                    for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
-            }
-            fence<T>();
-            // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory
-            if constexpr (!SAVE) {
-#pragma unroll
-                for (int i = 0; i < 6; ++i) pf[i] = p_row.frag(L::P + 16 * (i < 4 ? i : i - 2) * RC, i / 4);
+                for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], rd[4 * p + rt], p ? O[rt] : zero);
                 fence<T>();
 #pragma unroll
-                for (int p = 0; p < NT / 2; ++p) {
-#pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) O[rt] = mma(Sh[p], rd[4 * p + rt], p ? O[rt] : zero);
-                    fence<T>();
-#pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_cols(4 * p + rt);
-                    fence<T>();
-                }
+                for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_cols(4 * p + rt);
+                fence<T>();
             }
-            if constexpr (SAVE) {
+        };
+        if constexpr (KS > 1) {            // the other features' part of K S, and of this wave's tokens of Q S
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
-                    store_frag<T>((T*)a.z + (at * Dv + wg0 + col + m) * kChunk + 32 * b + 8 * grp, frag_of<T>(Z[2 * b], Z[2 * b + 1]));
-            }
-            F Uh[2], Ul[BF ? 2 : 1];
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] *= bt[rt];              // U
+            for (int rt = 0; rt < 4; ++rt) lds_write(mine + 1024 * rt, Z[rt]);
             if constexpr (!SAVE) {
+                q_state();
 #pragma unroll
-                for (int b = 0; b < 2; ++b) Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) O[rt] = times(O[rt], row_gam[rt]);
-#pragma unroll
-                for (int i = 0; i < 6; ++i) O[i < 4 ? i : i - 2] = mma(Uh[i / 4], pf[i], O[i < 4 ? i : i - 2]);
+                for (int i = 0; i < NO; ++i) lds_write(mine + 1024 * (4 + i), O[NO + i]);
             }
+            __syncthreads();
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Z[rt] *= en[rt];
+            for (int rt = 0; rt < 4; ++rt) Z[rt] += lds_read<f32x4>(others + 1024 * rt);
+            if constexpr (!SAVE)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
-                if constexpr (BF) Ul[b] = rest_of(Uh[b], Z[2 * b], Z[2 * b + 1]);
-            }
+                for (int i = 0; i < NO; ++i) O[i] += lds_read<f32x4>(others + 1024 * (4 + i));
+        }
+        if constexpr (BF && !SAVE)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int i = 0; i < 6; ++i) tl[i] = t_row.frag(L::T2, i < 4 ? i : i - 2, i / 4);
+        fence<T>();
 #pragma unroll
-                for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], Uh[b], S[t][c]);
-                if constexpr (BF)
+        for (int t = 0; t < NT; ++t) S[t] = times(S[t], whole);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], Ul[b], S[t][c]);
-            }
-            if constexpr (!SAVE) {
-                T* const out = (T*)a.o + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
-                if (rows == kChunk) {
+        for (int rt = 0; rt < 4; ++rt) Z[rt] = V[rt] - gam[rt] * Z[rt];
+        F Xh[2], Xl[BF ? 2 : 1];
 #pragma unroll
-                    for (int rt = 0; rt < 4; ++rt) store4(out + (size_t)(16 * rt) * Dv, O[rt]);
-                } else {
+        for (int b = 0; b < 2; ++b) {
+            Xh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
+            if constexpr (BF) Xl[b] = rest_of(Xh[b], Z[2 * b], Z[2 * b + 1]);
+        }
+        fence<T>();
 #pragma unroll
-                    for (int rt = 0; rt < 4; ++rt)
-                        if (16 * rt + m < rows) store4(out + (size_t)(16 * rt) * Dv, O[rt]);
-                }
+        for (int rt = 0; rt < 4; ++rt) {
+            bt[rt] = vec4(2, rt);
+            en[rt] = vec4(1, rt);
+            if (!SAVE && rt < NO) row_gam[rt] = lds_read<float>(vec + 4 * (m + 16 * part) + 64 * KS * rt) * a.scale;
+        }
+        fence<T>();
+#pragma unroll
+        for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
+        if constexpr (BF) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tf[i], Xl[i / 4], Z[i < 4 ? i : i - 2]);
+            if constexpr (!SAVE)
+#pragma unroll
+                for (int i = 0; i < 6; ++i) Z[i < 4 ? i : i - 2] = mma(tl[i], Xh[i / 4], Z[i < 4 ? i : i - 2]);
+        }
+        fence<T>();
+        // O transposed, its rows value columns and its columns tokens: a lane's values are neighbours in memory
+        if constexpr (!SAVE) {
+#pragma unroll
+            for (int i = 0; i < NO * 3 / 2; ++i) pf[i] = p_row.frag(L::P + 16 * KS * (i < NO ? i : i - NO / 2) * RC, i / NO);
+            fence<T>();
+            if constexpr (KS == 1) q_state();
+        }
+        if constexpr (SAVE) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                if (KS == 1 || b == part) store_frag<T>((T*)a.z + (at * Dv + wg0 + c0 + m) * kChunk + 32 * b + 8 * grp, frag_of<T>(Z[2 * b], Z[2 * b + 1]));
+        }
+        F Uh[2], Ul[BF ? 2 : 1];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) Z[rt] *= bt[rt];              // U
+        if constexpr (!SAVE) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
+#pragma unroll
+            for (int i = 0; i < NO; ++i) O[i] = times(O[i], row_gam[i]);
+#pragma unroll
+            for (int i = 0; i < NO * 3 / 2; ++i) O[i < NO ? i : i - NO / 2] = mma(Uh[i / NO], pf[i], O[i < NO ? i : i - NO / 2]);
+        }
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) Z[rt] *= en[rt];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            Uh[b] = frag_of<T>(Z[2 * b], Z[2 * b + 1]);
+            if constexpr (BF) Ul[b] = rest_of(Uh[b], Z[2 * b], Z[2 * b + 1]);
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t] = mma(rd[b * NT + t], Uh[b], S[t]);
+            if constexpr (BF)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) S[t] = mma(rd[b * NT + t], Ul[b], S[t]);
+        }
+        if constexpr (!SAVE) {
+            T* const out = (T*)a.o + (val_row + t0 + 16 * part + m) * Dv + wg0 + c0 + 4 * grp;
+            if (rows == kChunk) {
+#pragma unroll
+                for (int i = 0; i < NO; ++i) store4(out + (size_t)(16 * KS * i) * Dv, O[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NO; ++i)
+                    if (16 * (KS * i + part) + m < rows) store4(out + (size_t)(16 * KS * i) * Dv, O[i]);
             }
         }
         if constexpr (BF) {                // the other buffer
@@ -321,6 +355,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             t_row.move(by);
             v_col.move(by);
             q_row.move(by);
+            q_others.move(by);
             p_row.move(by);
             vec += by;
         } else {
@@ -328,22 +363,21 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         }
     }
     if (!SAVE && a.kv_out) {
-        float* const out = a.kv_out + (size_t)chain * DK * Dv + wg0 + c0 + m;
+        float* const out = a.kv_out + ((size_t)chain * DK + f0) * Dv + wg0 + c0 + m;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) out[(size_t)(token_of(t, grp) + i) * Dv + 16 * c] = S[t][c][i];
+            for (int i = 0; i < 4; ++i) out[(size_t)(token_of(t, grp) + i) * Dv] = S[t][i];
     }
 }
 
 // Backward, from the last chunk to the first: dV and the derivatives of the states behind chunks.
-template <class T, int DK, int CT, int W>
-__global__ __launch_bounds__(threads_of<T>(W)) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+template <class T, int DK, int KS>
+__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     constexpr bool BF = sizeof(T) == 2;
-    constexpr int COLS = 16 * CT * W, NT = DK / 16;
+    static_assert(KS == 1 || !BF, "the waves that fetch take no part in the exchange");
+    constexpr int COLS = 16 * W / KS, NT = DK / 16 / KS, NP = NT / 2;
     typedef typename El<T>::F F;
     typedef SweepLds<T, DK, COLS, true, false> L;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -354,17 +388,15 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
     const unsigned lds0 = lds_address(lds);
-    const int wg0 = split * COLS, c0 = 16 * CT * w;
+    const int wg0 = split * COLS, c0 = 16 * (w / KS), part = w % KS, f0 = part * (DK / KS);
     const size_t key_row = ((size_t)s.row * a.Hk + h / (a.H / a.Hk)) * a.N + s.first;
     const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first;
 
-    f32x4 S[NT][CT];                       // dS
+    f32x4 S[NT];                       // dS
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) S[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < NT; ++t) S[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int chunks = (s.len + kChunk - 1) / kChunk;
-    SweepFetch<T, DK, COLS, fetchers<T>(W), true, false> next;
+    SweepFetch<T, DK, COLS, true, false> next;
     auto fetch = [&](int chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         next.fetch(a, (size_t)(s.slot + chunk) * a.H + h, key_row + t0, val_row + t0, rows, Dv, wg0,
@@ -385,9 +417,14 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     ColReader<T, DK, true> k_col(first, lane);
     ColReader<T, kChunk, true> t_col(first, lane);
     ColReader<T, COLS, false> v_col(first, lane);
+    if constexpr (KS > 1) {
+        k_row.skip(NP * part);
+        k_col.skip(NP * part);
+    }
     unsigned vec = first + L::VEC;
     auto vec4 = [&](int which, int rt) { return lds_read<f32x4>(vec + 32 * grp + 4 * (which * kChunk + token_of(rt, 0))); };
-    const Turn<T> turn(lds0 + L::ALL + w * Turn<T>::BYTES, lane);
+    const Turn<T> turn(lds0 + L::ALL + w * Turn<T>::BYTES, lane, part);
+    const unsigned swap = lds0 + L::ALL + W * Turn<T>::BYTES + lane * 16, mine = swap + w * Swap<true>::BYTES, others = swap + (w ^ 1) * Swap<true>::BYTES;
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
         const int t0 = chunk * kChunk, rows = s.len - t0 < kChunk ? s.len - t0 : kChunk;
         const size_t at = (size_t)(s.slot + chunk) * a.H + h;
@@ -395,100 +432,103 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         __syncthreads();
         if (!BF && chunk) fetch(chunk - 1);
 
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+        F rd[2 * NT];                  // K's rows, then Q's columns, then K's
+        // dO's columns; columns of P and T': row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first
+        F gf[2], pf[6], tf[6];
+        f32x4 gam[4], en[4], bt[4], Y[4];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            const int col = c0 + 16 * c;
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            F rd[2 * NT];                  // K's rows, then Q's columns, then K's
-            // dO's columns; columns of P and T': row tiles 0 .. 3 of the second 32 rows, 0, 1 of the first
-            F gf[2], pf[6], tf[6];
-            f32x4 gam[4], en[4], bt[4], Y[4];
+        for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
+        const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
 #pragma unroll
-            for (int i = 0; i < 2 * NT; ++i) rd[i] = k_row.frag(L::K, i % 4, i / 4);
-            const float whole = lds_read<float>(vec + 4 * (kChunk - 1));
+        for (int b = 0; b < 2; ++b) gf[b] = v_col.frag(L::V, b, c0 / 16);
 #pragma unroll
-            for (int b = 0; b < 2; ++b) gf[b] = v_col.frag(L::V, b, col / 16);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                en[rt] = vec4(1, rt);
-                gam[rt] = vec4(0, rt);
-            }
-#pragma unroll
-            for (int i = 0; i < 6; ++i) pf[i] = t_col.frag(L::P, i < 4, i < 4 ? i : i - 4);
-            fence<T>();
-            F Sf[NT / 2];
-#pragma unroll
-            for (int p = 0; p < NT / 2; ++p) {
-                Sf[p] = frag_of<T>(S[2 * p][c], S[2 * p + 1][c]);
-                store_frag<T>((T*)a.ds + (at * Dv + wg0 + col + m) * DK + 32 * p + 8 * grp, Sf[p]);
-            }
-            fence<T>();
-#pragma unroll
-            for (int p = 0; p < NT / 2; ++p) {
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(rd[4 * p + rt], Sf[p], p ? Y[rt] : zero);
-                fence<T>();
-#pragma unroll
-                for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_col.frag(L::Q, (4 * p + rt) / NT, (4 * p + rt) % NT);
-                fence<T>();
-            }
-#pragma unroll
-            for (int i = 0; i < 6; ++i) tf[i] = t_col.frag(L::T1, i < 4, i < 4 ? i : i - 4);
-            fence<T>();
-            F of[2];                       // scale gam dO
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                f32x4 o0, o1;
-                values_of(gf[b], o0, o1);
-                of[b] = frag_of<T>(times(gam[2 * b] * o0, a.scale), times(gam[2 * b + 1] * o1, a.scale));
-            }
-#pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = times(S[t][c], whole);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Y[rt] *= en[rt];
-            fence<T>();
-#pragma unroll
-            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
-            fence<T>();
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[t], of[0], S[t][c]);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) rd[t] = k_col.frag(L::K, 0, t);
-            fence<T>();
-            F uf[2];
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) Y[rt] *= bt[rt];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) uf[b] = frag_of<T>(Y[2 * b], Y[2 * b + 1]);
-#pragma unroll
-            for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(tf[i], uf[i < 4], Y[i < 4 ? i : i - 4]);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[NT + t], of[1], S[t][c]);
-            fence<T>();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) rd[NT + t] = k_col.frag(L::K, 1, t);
-            fence<T>();
-            // dV, turned round in LDS for its rows in memory: written a column a lane, read four columns of a token a lane
-#pragma unroll
-            for (int b = 0; b < 2; ++b) turn.write(b, frag_of<T>(Y[2 * b], Y[2 * b + 1]));
-            F xf[2];                       // -gam dV
-#pragma unroll
-            for (int b = 0; b < 2; ++b) xf[b] = frag_of<T>(-gam[2 * b] * Y[2 * b], -gam[2 * b + 1] * Y[2 * b + 1]);
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) S[t][c] = mma(rd[b * NT + t], xf[b], S[t][c]);
-            T* const out = (T*)a.dv + (val_row + t0 + m) * Dv + wg0 + col + 4 * grp;
-            // (of one wave, and in order: no wait but the reads' own)
-            asm volatile("" ::: "memory");
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) turn.store(out + (size_t)(16 * rt) * Dv, rt, 16 * rt + m < rows);
+        for (int rt = 0; rt < 4; ++rt) {
+            en[rt] = vec4(1, rt);
+            gam[rt] = vec4(0, rt);
         }
+#pragma unroll
+        for (int i = 0; i < 6; ++i) pf[i] = t_col.frag(L::P, i < 4, i < 4 ? i : i - 4);
+        fence<T>();
+        F Sf[NP];
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            Sf[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
+            store_frag<T>((T*)a.ds + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sf[p]);
+        }
+        fence<T>();
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Y[rt] = mma(rd[4 * p + rt], Sf[p], p ? Y[rt] : zero);
+            fence<T>();
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) rd[4 * p + rt] = k_col.frag(L::Q, (4 * p + rt) / NT, (4 * p + rt) % NT);
+            fence<T>();
+        }
+        if constexpr (KS > 1) {            // the other features' part of K dS
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) lds_write(mine + 1024 * rt, Y[rt]);
+            __syncthreads();
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) Y[rt] += lds_read<f32x4>(others + 1024 * rt);
+        }
+#pragma unroll
+        for (int i = 0; i < 6; ++i) tf[i] = t_col.frag(L::T1, i < 4, i < 4 ? i : i - 4);
+        fence<T>();
+        F of[2];                       // scale gam dO
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            f32x4 o0, o1;
+            values_of(gf[b], o0, o1);
+            of[b] = frag_of<T>(times(gam[2 * b] * o0, a.scale), times(gam[2 * b + 1] * o1, a.scale));
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t] = times(S[t], whole);
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) Y[rt] *= en[rt];
+        fence<T>();
+#pragma unroll
+        for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(pf[i], gf[i < 4], Y[i < 4 ? i : i - 4]);
+        fence<T>();
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) bt[rt] = vec4(2, rt);
+        fence<T>();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t] = mma(rd[t], of[0], S[t]);
+        fence<T>();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) rd[t] = k_col.frag(L::K, 0, t);
+        fence<T>();
+        F uf[2];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) Y[rt] *= bt[rt];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) uf[b] = frag_of<T>(Y[2 * b], Y[2 * b + 1]);
+#pragma unroll
+        for (int i = 0; i < 6; ++i) Y[i < 4 ? i : i - 4] = mma(tf[i], uf[i < 4], Y[i < 4 ? i : i - 4]);
+        fence<T>();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) S[t] = mma(rd[NT + t], of[1], S[t]);
+        fence<T>();
+#pragma unroll
+        for (int t = 0; t < NT; ++t) rd[NT + t] = k_col.frag(L::K, 1, t);
+        fence<T>();
+        // dV, turned round in LDS for its rows in memory: written a column a lane, read four columns of a token a lane
+#pragma unroll
+        for (int b = 0; b < 2; ++b) turn.write(b, frag_of<T>(Y[2 * b], Y[2 * b + 1]));
+        F xf[2];                       // -gam dV
+#pragma unroll
+        for (int b = 0; b < 2; ++b) xf[b] = frag_of<T>(-gam[2 * b] * Y[2 * b], -gam[2 * b + 1] * Y[2 * b + 1]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) S[t] = mma(rd[b * NT + t], xf[b], S[t]);
+        T* const out = (T*)a.dv + (val_row + t0 + 16 * part + m) * Dv + wg0 + c0 + 4 * grp;
+        // (of one wave, and in order: no wait but the reads' own)
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 4 / KS; ++i) turn.store(out + (size_t)(16 * KS * i) * Dv, KS * i, 16 * (KS * i + part) + m < rows);
         if constexpr (BF) {
             const int by = chunk & 1 ? -L::BYTES : L::BYTES;
             k_row.move(by);
@@ -502,21 +542,33 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     }
 }
 
+template <class T, int DK, int KS, bool SAVE>
+hipError_t launch_fwd_ks(const DeltaArgs& a, int Dv, hipStream_t stream) {
+    constexpr int COLS = 16 * W / KS, LDS = SweepLds<T, DK, COLS, !SAVE, true>::ALL + (KS > 1 ? W * Swap<SAVE>::BYTES : 0);
+    static_assert(LDS <= 160 * 1024, "LDS");
+    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, KS, SAVE>), dim3((unsigned)((long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
+    return hipGetLastError();
+}
+template <class T, int DK, int KS>
+hipError_t launch_bwd_ks(const DeltaArgs& a, int Dv, hipStream_t stream) {
+    constexpr int COLS = 16 * W / KS, LDS = SweepLds<T, DK, COLS, true, false>::ALL + W * (Turn<T>::BYTES + (KS > 1 ? Swap<true>::BYTES : 0));
+    static_assert(LDS <= 160 * 1024, "LDS");
+    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, KS>), dim3((unsigned)((long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
+    return hipGetLastError();
+}
+// fp32, while that leaves no workgroup without a compute unit of its own: two waves share 16 columns.
+bool shared_columns(const DeltaArgs& a, int Dv) { return (long long)a.seqs * a.H * (Dv / (16 * W)) * 2 <= 256; }
 template <class T, int DK, bool SAVE>
 hipError_t launch_fwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
-    constexpr int CT = 1, W = 4;
-    const int per = Dv / (16 * CT * W);
-    typedef SweepLds<T, DK, 16 * CT * W, !SAVE, true> L;
-    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, CT, W, SAVE>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL, stream, a, Dv, per);
-    return hipGetLastError();
+    if constexpr (sizeof(T) == 4)
+        if (shared_columns(a, Dv)) return launch_fwd_ks<T, DK, 2, SAVE>(a, Dv, stream);
+    return launch_fwd_ks<T, DK, 1, SAVE>(a, Dv, stream);
 }
 template <class T, int DK>
 hipError_t launch_bwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
-    constexpr int CT = 1, W = 4;
-    const int per = Dv / (16 * CT * W);
-    typedef SweepLds<T, DK, 16 * CT * W, true, false> L;
-    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, CT, W>), dim3((unsigned)((long long)a.seqs * a.H * per)), dim3(threads_of<T>(W)), L::ALL + W * Turn<T>::BYTES, stream, a, Dv, per);
-    return hipGetLastError();
+    if constexpr (sizeof(T) == 4)
+        if (shared_columns(a, Dv)) return launch_bwd_ks<T, DK, 2>(a, Dv, stream);
+    return launch_bwd_ks<T, DK, 1>(a, Dv, stream);
 }
 
 }  // namespace
