@@ -348,10 +348,11 @@ ltn_status ltn_attn_decode_steps_dkdv(const void* q, const void* k, const void* 
  *                 as it was.  Values are not read on the host; whatever they are, no access leaves the tensors (sequences
  *                 that they make overlap have undefined results).  seqs is not used without cu
  *   workspace   : device scratch of ltn_delta_workspace_bytes(..., call = 0) bytes
- * (Dk, Dv) in {64,128} x {64,128}; N < 2^31 - 64.  fp32 tensors: fp32 arithmetic throughout.  bf16 tensors: bf16 matrix
- * products with fp32 sums; what enters the state enters in two bf16 parts, so that kv_out is exact to about 4e-6 of
- * its norm, not to a bf16 rounding; o is rounded to bf16.  An infinity or NaN in a token reaches the later tokens of its
- * sequence, and may reach the other tokens of its chunk of 64.
+ * (Dk, Dv) in {64,128} x {64,128}; N <= 2^31 - 65, fewer than 2^22 sequences x value heads and 2^23 chunks x value heads
+ * (LTN_ERR_SHAPE).  fp32 tensors: fp32 arithmetic throughout; the order of a sum may depend on how many sequences and heads a
+ * call has.  bf16 tensors: bf16 matrix products with fp32 sums; what enters the state enters in two bf16 parts, so that
+ * kv_out is exact to about 4e-6 of its norm, not to a bf16 rounding; o is rounded to bf16.  An infinity or NaN in a token
+ * reaches the later tokens of its sequence, and may reach the other tokens of its chunk of 64; the gradients of the sequence.
  * N == 0 (or an empty sequence) hands kv_in (or zeros) on to kv_out.
  */
 ltn_status ltn_delta_fwd(const void* q, const void* k, const void* v, void* o, const float* g, const float* beta,
@@ -367,7 +368,7 @@ ltn_status ltn_delta_fwd(const void* q, const void* k, const void* v, void* o, c
  *   dv        out : device, [Bt,H,N,Dv] dtype
  *   dg, dbeta out : device, [Bt,H,N] dtype (the tensors' type: with bf16 tensors they are sums of bf16 products, and as exact)
  *   workspace     : device scratch of ltn_delta_workspace_bytes(..., call = 1) bytes; per 64 tokens and value head it holds,
- *                   among others, the state before them and its derivative behind them (7B-shaped layer: 2.2 GB)
+ *                   among others, the state before them and its derivative behind them (7B-shaped layer: 1.6 GB)
  * Other arguments, packed sequences and shapes as above.
  */
 ltn_status ltn_delta_bwd(const void* q, const void* k, const void* v, const void* d_o,

@@ -37,6 +37,9 @@ ltn_status check_delta(int Bt, int Hk, int H, long long N, int Dk, int Dv, bool 
     return LTN_OK;
 }
 
+// A launch has at most 2^32 threads in its grid: the sweeps up to 1024 a chain, "grad" 512 a chunk and head.
+bool launches(const DeltaDims& d, int H) { return d.chains < (1 << 22) && d.slots * H < (1 << 23); }
+
 // Hands out the workspace's arrays; returns its size.
 size_t lay_out(ltn::DeltaArgs& a, char* base, int Dk, int Dv, bool bf16, bool bwd) {
     const ltn::DeltaScratch s = ltn::delta_scratch(Dk, Dv, bf16);
@@ -64,7 +67,7 @@ size_t lay_out(ltn::DeltaArgs& a, char* base, int Dk, int Dv, bool bf16, bool bw
 size_t ltn_delta_workspace_bytes(int Bt, int H, long long N, int Dk, int Dv, int seqs, ltn_dtype dtype, int call) {
     if (Bt <= 0 || H <= 0 || N <= 0 || seqs < 0 || call < 0 || call > 1) return 0;
     DeltaDims d;
-    if (check_delta(Bt, H, H, N, Dk, Dv, seqs > 0, seqs, dtype, &d) != LTN_OK) return 0;
+    if (check_delta(Bt, H, H, N, Dk, Dv, seqs > 0, seqs, dtype, &d) != LTN_OK || !launches(d, H)) return 0;
     return (size_t)d.slots * H * ltn::delta_bytes(Dk, Dv, dtype == LTN_BF16, call == 1);
 }
 
@@ -75,6 +78,7 @@ ltn_status ltn_delta_fwd(const void* q, const void* k, const void* v, void* o, c
     DeltaDims d;
     const ltn_status cs = check_delta(Bt, Hk, H, N, Dk, Dv, cu != nullptr, seqs, dtype, &d);
     if (cs != LTN_OK) return cs;
+    if (!launches(d, H)) return LTN_ERR_SHAPE;
     const bool empty = Bt == 0 || H == 0 || N == 0;
     if (!empty && any_null(q, k, v, (const void*)o, (const void*)g, (const void*)beta)) return LTN_ERR_NULL;
     const size_t need = ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, cu ? seqs : 0, dtype, 0);
@@ -115,6 +119,7 @@ ltn_status ltn_delta_bwd(const void* q, const void* k, const void* v, const void
     DeltaDims d;
     const ltn_status cs = check_delta(Bt, Hk, H, N, Dk, Dv, cu != nullptr, seqs, dtype, &d);
     if (cs != LTN_OK) return cs;
+    if (!launches(d, H)) return LTN_ERR_SHAPE;
     const bool empty = Bt == 0 || H == 0 || N == 0;
     if (!empty && any_null(q, k, v, d_o, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)dg, (const void*)dbeta,
                            (const void*)g, (const void*)beta))

@@ -142,3 +142,14 @@ def test_the_reference_against_differences():
         assert torch.isclose(slope, (grads[i] * step).sum(), rtol=1e-6, atol=1e-14)
     x, y, gate, w = (torch.randn(s, dtype=torch.float64, requires_grad=True) for s in ((4, 6), (4, 6), (2, 6), (6,)))
     assert torch.autograd.gradcheck(lambda x, y, g, w: block_norm(x, y, g, w, w * 2, 0.7, 1e-5, True), (x, y, gate, w))
+
+
+@pytest.mark.parametrize("call", [fwd, bwd])
+def test_more_than_a_launch_holds_is_refused(lib, call):
+    big = dict(ws_bytes=1 << 60, q=1 << 50, ws=1 << 60)
+    assert call(lib, Bt=1 << 21, N=1, **big) == E_SHAPE                             # 2^22 chains
+    assert call(lib, N=1 << 28, **big) == E_SHAPE                                   # 2^23 chunks and heads
+    assert call(lib, cu=15 * G, seqs=1 << 21, N=1, **big) == E_SHAPE
+    assert ltn.ltn_delta_workspace_bytes(1 << 21, 2, 1, 64, 64, 0, torch.bfloat16, 0) == 0
+    assert ltn.ltn_delta_workspace_bytes(1, 2, 1 << 28, 64, 64, 0, torch.bfloat16, 0) == 0
+    assert ltn.ltn_delta_workspace_bytes(1, 2, (1 << 28) - 64, 64, 64, 0, torch.bfloat16, 0) > 0
