@@ -154,11 +154,9 @@ __device__ __forceinline__ bf16x8 rest_of(const bf16x8& f, const f32x4& x, const
     f32x4 a, b;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {          // (from the packed words: the compiler would convert each value again)
-        unsigned word = h.u[i];
-        asm("" : "+v"(word));
         f32x4& r = i < 2 ? a : b;
-        r[2 * (i & 1)] = __uint_as_float(word << 16);
-        r[2 * (i & 1) + 1] = __uint_as_float(word & 0xffff0000u);
+        asm("v_lshlrev_b32 %0, 16, %1" : "=v"(r[2 * (i & 1)]) : "v"(h.u[i]));
+        asm("v_and_b32 %0, 0xffff0000, %1" : "=v"(r[2 * (i & 1) + 1]) : "v"(h.u[i]));
     }
     return frag_of<__bf16>(x - a, y - b);
 }
@@ -301,14 +299,15 @@ template <class T, int COLS, bool PAIRED> struct ColReader {
 
 // A tile from global memory, rows `pitch` bytes apart, by W waves; rows from `valid` on become zero.  bf16: fetch() issues
 // direct loads to LDS and the data is there once they have been waited for.  fp32: fetch() loads registers, put() stores them.
-template <class T, int COLS, int W, int ROWS = kChunk> struct TileFetch;
-template <int COLS, int W, int ROWS> struct TileFetch<__bf16, COLS, W, ROWS> {
+template <class T, int COLS, int W, int ROWS = kChunk, bool KEEP = false> struct TileFetch;
+template <int COLS, int W, int ROWS, bool KEEP> struct TileFetch<__bf16, COLS, W, ROWS, KEEP> {
     typedef Swz<COLS> S;
     static constexpr int NV = S::CPR / 4, NI = S::NI * ROWS / kChunk, PER = NI / W;      // loads of a tile and of a wave
     static_assert(NI % W == 0 && NV >= 1, "every wave issues the same number of loads");
     // src: wave-uniform
     __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, unsigned lds, int w, int lane) {
-        const int own = (int)hide((unsigned)lane);     // (offsets formed at each fetch: registers are dearer from chunk to chunk)
+        // KEEP: the lane's offsets are formed once, in registers; else at each fetch (where waves that fetch compute too, registers are dearer)
+        const int own = KEEP ? lane : (int)hide((unsigned)lane);
         if (valid >= ROWS) {               // a scalar base and the lane's offset, the same for each load where its rows are 16 n apart
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
@@ -327,7 +326,7 @@ template <int COLS, int W, int ROWS> struct TileFetch<__bf16, COLS, W, ROWS> {
     }
     __device__ __forceinline__ void put(unsigned, int, int) const {}
 };
-template <int COLS, int W, int ROWS> struct TileFetch<float, COLS, W, ROWS> {
+template <int COLS, int W, int ROWS, bool KEEP> struct TileFetch<float, COLS, W, ROWS, KEEP> {
     static constexpr int CPR = COLS / 4, PER = ROWS * CPR / (64 * W);
     u32x4 v[PER];
     __device__ __forceinline__ void fetch(const char* src, unsigned pitch, int valid, unsigned, int w, int lane) {

@@ -94,9 +94,9 @@ template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepFetch {
     typedef SweepLds<T, DK, COLS, FULL, FWD> L;
     static constexpr bool BF = sizeof(T) == 2;
     static constexpr size_t kTile = (size_t)kChunk * kChunk * sizeof(T);
-    TileFetch<T, DK, W> k, q;
-    TileFetch<T, kChunk, W> t1, t2, p;
-    TileFetch<T, COLS, W> v;
+    TileFetch<T, DK, W, kChunk, true> k, q;
+    TileFetch<T, kChunk, W, kChunk, true> t1, t2, p;
+    TileFetch<T, COLS, W, kChunk, true> v;
     u32x4 vec;
     // at: the chunk's scratch; key_row, val_row: its first token's rows
     __device__ __forceinline__ void fetch(const DeltaArgs& a, size_t at, size_t key_row, size_t val_row, int rows, int Dv, int col0,
@@ -176,7 +176,22 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) S[t][i] = in[(size_t)(token_of(t, grp) + i) * Dv];   // (features are dealt as tokens)
     }
+    // The state as an operand, and into memory.  Behind a chunk and not before the next: there the stores would wait until the
+    // next tiles' loads have been issued, which keep the memory path busy for 1300 cycles and more.
+    F Sh[NP], Sl[BF ? NP : 1];
+    auto hand_on = [&](size_t at, bool chunk_there) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            Sh[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
+            if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p], S[2 * p + 1]);
+        }
+        if constexpr (SAVE)
+            if (chunk_there)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sh[p]);
+    };
     if (!BF && chunks) fetch(0);
+    if (BF && chunks) hand_on((size_t)s.slot * a.H + h, true);
     PairedRowReader<T, DK> k_row(lds0, lane);
     ColReader<T, DK, true> k_col(lds0, lane);
     PairedRowReader<T, kChunk> t_row(lds0, lane);
@@ -218,14 +233,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
         for (int i = 0; i < 6; ++i) tf[i] = t_row.frag(L::T1, i < 4 ? i : i - 2, i / 4);
         fence<T>();
-        F Sh[NP], Sl[BF ? NP : 1];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            Sh[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
-            if constexpr (BF) Sl[p] = rest_of(Sh[p], S[2 * p], S[2 * p + 1]);
-            if constexpr (SAVE) store_frag<T>((T*)a.s0 + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sh[p]);
-        }
-        fence<T>();
+        if constexpr (!BF) hand_on(at, true);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
 #pragma unroll
@@ -349,6 +357,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
             }
         }
         if constexpr (BF) {                // the other buffer
+            hand_on(at + a.H, chunk + 1 < chunks);
             const int by = chunk & 1 ? -L::BYTES : L::BYTES;
             k_row.move(by);
             k_col.move(by);
@@ -411,7 +420,16 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
         }
         return;
     }
+    F Sf[NP];
+    auto hand_on = [&](size_t at, bool chunk_there) {      // (as in the forward)
+#pragma unroll
+        for (int p = 0; p < NP; ++p) Sf[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
+        if (chunk_there)
+#pragma unroll
+            for (int p = 0; p < NP; ++p) store_frag<T>((T*)a.ds + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sf[p]);
+    };
     if (!BF && chunks) fetch(chunks - 1);
+    if (BF && chunks) hand_on((size_t)(s.slot + chunks - 1) * a.H + h, true);
     const unsigned first = lds0 + (BF && (chunks - 1) & 1 ? L::BYTES : 0);
     PairedRowReader<T, DK> k_row(first, lane);
     ColReader<T, DK, true> k_col(first, lane);
@@ -450,13 +468,7 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
         for (int i = 0; i < 6; ++i) pf[i] = t_col.frag(L::P, i < 4, i < 4 ? i : i - 4);
         fence<T>();
-        F Sf[NP];
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-            Sf[p] = frag_of<T>(S[2 * p], S[2 * p + 1]);
-            store_frag<T>((T*)a.ds + (at * Dv + wg0 + c0 + m) * DK + f0 + 32 * p + 8 * grp, Sf[p]);
-        }
-        fence<T>();
+        if constexpr (!BF) hand_on(at, true);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
 #pragma unroll
@@ -530,6 +542,7 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 #pragma unroll
         for (int i = 0; i < 4 / KS; ++i) turn.store(out + (size_t)(16 * KS * i) * Dv, KS * i, 16 * (KS * i + part) + m < rows);
         if constexpr (BF) {
+            hand_on(at - a.H, chunk > 0);
             const int by = chunk & 1 ? -L::BYTES : L::BYTES;
             k_row.move(by);
             k_col.move(by);
