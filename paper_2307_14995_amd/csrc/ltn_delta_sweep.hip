@@ -19,9 +19,11 @@
 // Q S through LDS.  Two rows of 700 tokens, 8 heads of 64: forward 75 -> 60 us, the gradients' sweeps 53 -> 40 and 84 ->
 // 67.  (bf16 gains nothing from it: one prompt of 3001 tokens 116 us either way.)
 //
-// What bounds them, heads of 128 features: 256 or more workgroups, HBM (4 rows of 8192 tokens, 32 heads, bf16: forward 326
-// us at 4.4 TB/s, the gradients' two 312 and 425); fewer, a chunk's chain of dependent steps, 1.9 to 2.4 us, in which LDS
-// serves 340 KB of operands (3100 of 4700 cycles; matrix products take 1700): one prompt of 3001 tokens, 47 chunks, 96 us.
+// What bounds them, heads of 128 features: 256 or more workgroups, HBM (4 rows of 8192 tokens, 32 heads, bf16: forward 316
+// us at 4.6 TB/s, the gradients' two 290 and 375 at 4.9); fewer, a chunk's chain of dependent steps, 1.9 to 2.4 us: of the
+// forward's 4500 cycles matrix products take 1660 and vector instructions 1990, which one wave a SIMD hardly overlaps
+// (asked to interleave them, the compiler ran out of registers: 128 us for 70), and LDS is busy 1580.  One prompt of 3001
+// tokens, 47 chunks, 91 us; 8 rows of 2048 tokens, 8 heads: 68, 61 and 76 us.
 #include "ltn_delta.h"
 
 namespace ltn {
