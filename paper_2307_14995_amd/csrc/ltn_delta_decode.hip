@@ -5,6 +5,9 @@
 //     u = beta (v - A^T k),   S = A + k u^T,   o = scale (A^T q + (q . k) u),
 //
 // so both sums over rows are taken in one pass over A and meet once.
+// Bound by HBM for a batch: 2048 states of 128 x 128 53.7 us (5.05 TB/s; 41 where the memory-side cache holds them); one
+// sequence of 32 heads by the host's call, 5.6 us, of which the kernel takes 3.6.  Slices of 32 columns make four workgroups a
+// state of 128 x 128, enough of them for one sequence.
 #include "ltn_delta.h"
 
 namespace ltn {

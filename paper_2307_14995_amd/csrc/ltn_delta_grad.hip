@@ -1,9 +1,13 @@
 // Gated delta rule: the gradients of a chunk of 64 tokens and a head of keys (ltn_delta.h has the formulas), from Z, dV and
 // the states that the sweeps left.  The value heads that share the keys follow one another in one workgroup: their dq and
-// dk are summed in registers, in a fixed order.  Wave w owns tokens 16 (w % 4) .. +15 and half of the
-// key features; the value features come in slabs of VS, so that
-// two workgroups fit a compute unit and one's loads pass while the other computes.
-// Scales of rows and columns (decays, beta) are applied to products' fp32 results, never to an operand.
+// dk are summed in registers, in a fixed order.  Wave w owns tokens 16 (w % 4) .. +15 and half of the key features; the
+// value features come in slabs of VS, so that two workgroups fit a compute unit (62 KB of LDS; 128 registers where a value head
+// has its keys alone) and one's loads pass while the other computes.
+// Scales of rows and columns (decays, beta) are applied to products' fp32 results, never to an operand.  What is rounded to
+// bf16 are dP and E as operands of the products with K and Q; the row and column sums that dg and dbeta take are of dP and E
+// in fp32 (a decay's gradient is a small difference of large sums: 1.5e-2 off for keys that are alike, with rounded ones).
+// Bound by HBM where the card is full: 178 KB a chunk and head, of which the two states are 64; 4 rows of 8192 tokens, 32 heads
+// of 128 features, bf16: 640 us, 4.6 TB/s.  8 rows of 2048, 8 heads on 4 key heads: 102 us.
 #include "ltn_delta.h"
 
 namespace ltn {

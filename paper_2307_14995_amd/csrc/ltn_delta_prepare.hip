@@ -4,8 +4,10 @@
 // Q K^T and K K^T are taken transposed: a lane holds four neighbours of one token's row, which go to memory (P) and to LDS
 // (L) as they are.  The inverse is taken in fp32 whatever the tensors' type: blocks of 16 on the diagonal by substitution, a
 // lane a column; then pairs of blocks are merged, T21 = -T22 (A21 T11), to 32 and to 64 with fp32 matrix instructions.
-// (Substitution and merging are as exact for keys that are alike, where powers of L grow before they vanish.)
-// Little work between loads and stores, in steps that wait for each other: what counts is how many workgroups a unit holds.
+// (Keys that repeat are why it is not a product of powers: those of L grow before they vanish.)
+// Little work between loads and stores, in steps that wait for each other: what counts is how many workgroups a unit holds,
+// three at 35 KB of LDS and 104 registers.  4 rows of 8192 tokens, 32 heads of 128 features, bf16: 173 us, 4.8 (gradients: T'
+// in one part) to 5.5 TB/s of q, k, T' and P, about a copy's rate; 47 chunks of 32 heads, which do not fill the card, 24 us.
 #include "ltn_delta.h"
 
 namespace ltn {
