@@ -684,6 +684,12 @@ def ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, dtype, call) -> int:
                                                         _dtype_code(dtype), int(call)))
 
 
+def _one_gpu(device, *tensors):
+    """All of `tensors` (None: not given) live on `device`; else the library would write to memory that is not its GPU's."""
+    if any(t is not None and t.device != device for t in tensors):
+        raise ValueError("all tensors must live on one GPU")
+
+
 def _check_delta(q, k, v, g, beta, cu):
     """(Bt, Hk, H, N, Dk, Dv, packed sequences or 0, rows of states)."""
     _devs("q k v g beta", q, k, v, g, beta)
@@ -705,8 +711,7 @@ def _check_delta(q, k, v, g, beta, cu):
         if cu.dtype != torch.int32 or cu.dim() != 1 or cu.numel() < 2 or Bt != 1:
             raise ValueError("cu must be int32 [seqs + 1] over tensors with Bt = 1")
         seqs = rows = cu.numel() - 1
-    if any(t.device != q.device for t in (k, v, g, beta) + (() if cu is None else (cu,))):
-        raise ValueError("all tensors must live on one GPU")
+    _one_gpu(q.device, k, v, g, beta, cu)
     return Bt, Hk, H, N, Dk, Dv, seqs, rows
 
 
@@ -727,6 +732,7 @@ def ltn_delta_fwd(q, k, v, g, beta, kv_in=None, cu=None, scale=1.0, return_state
         _out(kv_out, "kv_out", rows * H * Dk * Dv, torch.float32)
     elif return_state:
         kv_out = torch.empty((rows, H, Dk, Dv), dtype=torch.float32, device=q.device)
+    _one_gpu(q.device, o, kv_in, kv_out)
     code = _dtype_code(q.dtype)
     ws_bytes = int(lib.ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, code, 0))
     ws = _workspace(ws_bytes, q.device)
@@ -753,6 +759,7 @@ def ltn_delta_bwd(q, k, v, g, beta, d_o, cu=None, scale=1.0, out=None):
         dq, dk, dv, dg, dbeta = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), dg, torch.empty_like(dg)
     else:
         dq, dk, dv, dg, dbeta = (_out(t, "out", n, q.dtype) for t, n in zip(out, (q.numel(), k.numel(), v.numel(), g.numel(), g.numel())))
+        _one_gpu(q.device, dq, dk, dv, dg, dbeta)
     code = _dtype_code(q.dtype)
     ws_bytes = int(lib.ltn_delta_workspace_bytes(Bt, H, N, Dk, Dv, seqs, code, 1))
     ws = _workspace(ws_bytes, q.device)
@@ -774,6 +781,7 @@ def ltn_delta_decode_steps(q, k, v, kv, g, beta, scale=1.0, out=None):
     if kv.dtype != torch.float32 or tuple(kv.shape) != (Bt, H, Dk, Dv) or kv.device != q.device:
         raise ValueError("kv must be fp32 [Bt,H,Dk,Dv] on q's device")
     o = torch.empty_like(v) if out is None else _out(out, "out", v.numel(), v.dtype)
+    _one_gpu(q.device, o)
     rc = _call(lib.ltn_delta_decode_steps, q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(kv), _ptr(g), _ptr(beta),
                float(scale), Bt, Hk, H, S, Dk, Dv, _dtype_code(q.dtype))
     if rc != 0:
@@ -809,8 +817,7 @@ def _check_block_norm(x, y, gate, w_after, w_before, after, others=()):
             gates *= n
         if gates == 0 or rows % gates:
             raise ValueError("the rows of x must be a multiple of those of gate")
-    if any(t is not None and t.device != x.device for t in (y, gate, w_after, w_before, *(t for _, t in others))):
-        raise ValueError("all tensors must live on one GPU")
+    _one_gpu(x.device, y, gate, w_after, w_before, *(t for _, t in others))
     return rows, gates, C
 
 
@@ -827,6 +834,7 @@ def ltn_block_norm_fwd(x, y, gate=None, w_after=None, w_before=None, scale=1.0, 
         xo, h = torch.empty_like(x), torch.empty_like(x)
     else:
         xo, h = (_out(t, "out", x.numel(), x.dtype) for t in out)
+        _one_gpu(x.device, xo, h)
     rc = _call(lib.ltn_block_norm_fwd, x.device, _ptr(x), _ptr(y), _ptr(gate), _ptr(w_after), _ptr(w_before), _ptr(xo), _ptr(h),
                float(scale), float(eps), int(bool(after)), rows, gates, C, _dtype_code(x.dtype))
     if rc != 0:

@@ -153,3 +153,35 @@ def test_more_than_a_launch_holds_is_refused(lib, call):
     assert ltn.ltn_delta_workspace_bytes(1 << 21, 2, 1, 64, 64, 0, torch.bfloat16, 0) == 0
     assert ltn.ltn_delta_workspace_bytes(1, 2, 1 << 28, 64, 64, 0, torch.bfloat16, 0) == 0
     assert ltn.ltn_delta_workspace_bytes(1, 2, (1 << 28) - 64, 64, 64, 0, torch.bfloat16, 0) > 0
+
+
+class Stub:
+    """A tensor as the binding's checks see one, on a GPU that need not exist."""
+
+    def __init__(self, index, dtype, *shape):
+        self.device, self.dtype, self.shape, self.is_cuda = torch.device("cuda", index), dtype, torch.Size(shape), True
+
+    dim = lambda self: len(self.shape)
+    numel = lambda self: self.shape.numel()
+    is_contiguous = lambda self: True
+
+
+def test_an_output_on_another_gpu_is_refused(monkeypatch):
+    from paper_2307_14995_amd import binding
+
+    class NoFast:                          # (its marshalling passes on what it does not take)
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(binding, "_fast", NoFast)
+    bf, f32 = torch.bfloat16, torch.float32
+    q, v, g, s, x = Stub(0, bf, 1, 2, 8, 64), Stub(0, bf, 1, 2, 8, 64), Stub(0, f32, 1, 2, 8), Stub(0, f32, 1, 2, 64, 64), Stub(0, bf, 8, 64)
+    v1, g1, s1, x1 = (Stub(1, t.dtype, *t.shape) for t in (v, g, s, x))
+    dg = Stub(0, bf, 1, 2, 8)
+    for fn in (lambda: ltn.ltn_delta_fwd(q, q, v, g, g, out=v1), lambda: ltn.ltn_delta_fwd(q, q, v, g, g, kv_in=s1, out=v),
+               lambda: ltn.ltn_delta_fwd(q, q, v, g, g, kv_out=s1, out=v), lambda: ltn.ltn_delta_fwd(q, q, v1, g, g, out=v),
+               lambda: ltn.ltn_delta_bwd(q, q, v, g, g, v, out=(q, q, v, dg, Stub(1, bf, 1, 2, 8))),
+               lambda: ltn.ltn_delta_decode_steps(q, q, v, s, g, g, out=v1), lambda: ltn.ltn_delta_decode_steps(q, q, v, s, g1, g, out=v),
+               lambda: ltn.ltn_block_norm_fwd(x, x, out=(x, x1))):
+        with pytest.raises(ValueError, match="one GPU"):
+            fn()
