@@ -65,7 +65,7 @@ def algorithmic_bytes_per_token_head(D: int, esize: int):
 
 # What the timed calls launch, what that includes, and where it is chosen
 TIMED_SOURCES = ("ltn_pass_bf16.hip", "ltn_pass_f32.hip", "ltn_scan.hip", "ltn_bf16_tiles.h", "ltn_cache.h", "ltn_kernels.h",
-                 "ltn_api.hip")
+                 "ltn_args.h", "ltn_api.hip")
 
 
 def kernel_source_hash() -> str:
