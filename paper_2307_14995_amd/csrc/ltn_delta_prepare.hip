@@ -6,8 +6,8 @@
 // lane a column; then pairs of blocks are merged, T21 = -T22 (A21 T11), to 32 and to 64 with fp32 matrix instructions.
 // (Keys that repeat are why it is not a product of powers: those of L grow before they vanish.)
 // Little work between loads and stores, in steps that wait for each other: what counts is how many workgroups a unit holds,
-// three at 35 KB of LDS and 104 registers.  4 rows of 8192 tokens, 32 heads of 128 features, bf16: 173 us, 4.8 (gradients: T'
-// in one part) to 5.5 TB/s of q, k, T' and P, about a copy's rate; 47 chunks of 32 heads, which do not fill the card, 24 us.
+// four at 35 KB of LDS and 119 registers.  4 rows of 8192 tokens, 32 heads of 128 features, bf16: 161 us at 5.0 (gradients: T'
+// in one part) to 5.8 TB/s of q, k, T' and P, a copy's rate; 47 chunks of 32 heads, two rounds of workgroups, 22 us.
 #include "ltn_delta.h"
 
 namespace ltn {
@@ -29,6 +29,8 @@ template <class T, int DK> struct PrepareLds {
     static constexpr int INV = kChunk * LA * 4, KB = Tile<T, DK>::BYTES > INV ? Tile<T, DK>::BYTES : INV;
     static constexpr int L = KB, BYTES = KB + INV;                       // K, later the inverse; L
 };
+
+constexpr double kLog2e = 1.4426950408889634;
 
 template <class T, int DK>
 __global__ __launch_bounds__(kThreads, 3)
@@ -54,29 +56,29 @@ void delta_prepare_kernel(DeltaArgs a) {
     const int r = 16 * w + m;              // the lane's token
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
-    TileFetch<T, DK, 4> k;
-    k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base, w, lane);
+    // (in this order: loads come back in theirs, and the decays are worked on while K is still on its way)
+    float gl = 0.f, b = 0.f;
+    if (w == 0 && lane < rows) {
+        gl = a.g[gate_row + lane];
+        b = a.beta[gate_row + lane];
+    }
     F q[DK / 32];
     {
         const T* const row = (const T*)a.q + (key_row + (r < rows ? r : 0)) * DK + 8 * grp;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) q[kb] = *(const F*)(row + 32 * kb);
     }
+    TileFetch<T, DK, 4> k;
+    k.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base, w, lane);
     if (w == 0) {
         // log decays below -200 (exp underflows from -104 on) count as -200: sums of them stay finite, an infinite one's too
-        double x = 0.0;
-        float b = 0.f;
-        if (lane < rows) {
-            const float gl = a.g[gate_row + lane];
-            x = gl < -200.f ? -200.0 : (double)gl;
-            b = a.beta[gate_row + lane];
-        }
+        double x = gl < -200.f ? -200.0 : (double)gl;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const double y = __shfl_up(x, d, 64);
             if (lane >= d) x += y;
         }
-        G[lane] = x;
+        G[lane] = x * kLog2e;
         B[lane] = b;
         const double last = __shfl(x, 63, 64);
         float* const vec = a.vec + at * kVec;
@@ -116,7 +118,7 @@ void delta_prepare_kernel(DeltaArgs a) {
             f32x4 x, y;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float ratio = expf((float)(gr - G[c + i]));
+                const float ratio = __builtin_amdgcn_exp2f((float)(gr - G[c + i]));    // (a rounding as large as that of an exponent to e)
                 x[i] = r > c + i ? ratio * kk[ct][i] : 0.f;
                 y[i] = r >= c + i && r < rows ? a.scale * ratio * qk[ct][i] : 0.f;
             }
@@ -126,17 +128,22 @@ void delta_prepare_kernel(DeltaArgs a) {
     }
     __syncthreads();                       // L is there, and K is read: the inverse takes its place
 
-    if (lane < 16) {                       // block w of the diagonal, column m
+    if (lane < 16) {                       // block w of the diagonal, column m: each row's result goes into all rows below at once
         const float* const Lb = L + 16 * w * LA + 16 * w;
         const float* const bb = B + 16 * w;
-        float x[16], y[16];
+        f32x4 l[16][4];
+        float x[16];
 #pragma unroll
         for (int n = 0; n < 16; ++n) {
-            float sum = 0.f;
+            x[n] = n == m ? 1.f : 0.f;
 #pragma unroll
-            for (int i = 0; i < n; ++i) sum = fmaf(Lb[n * LA + i], y[i], sum);
-            x[n] = (n == m ? 1.f : 0.f) - sum;
-            y[n] = bb[n] * x[n];
+            for (int i = 0; 4 * i < n; ++i) l[n][i] = *(const f32x4*)(Lb + n * LA + 4 * i);
+        }
+#pragma unroll
+        for (int i = 0; i < 15; ++i) {
+            const float y = -bb[i] * x[i];
+#pragma unroll
+            for (int n = i + 1; n < 16; ++n) x[n] = fmaf(l[n][i / 4][i % 4], y, x[n]);
         }
 #pragma unroll
         for (int n = 0; n < 16; ++n) Tm[(16 * w + n) * LA + 16 * w + m] = x[n];
