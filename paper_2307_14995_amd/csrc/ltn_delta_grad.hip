@@ -7,7 +7,8 @@
 // bf16 are dP and E as operands of the products with K and Q; the row and column sums that dg and dbeta take are of dP and E
 // in fp32 (a decay's gradient is a small difference of large sums: 1.5e-2 off for keys that are alike, with rounded ones).
 // Bound by HBM where the card is full: 178 KB a chunk and head, of which the two states are 64; 4 rows of 8192 tokens, 32 heads
-// of 128 features, bf16: 640 us, 4.6 TB/s.  8 rows of 2048, 8 heads on 4 key heads: 102 us.
+// of 128 features, bf16: 600 us, 4.9 TB/s.  8 rows of 2048, 8 heads on 4 key heads, a workgroup a unit: 94 us (104 where each
+// head fetched K, Q and its slabs when it came to them).
 #include "ltn_delta.h"
 
 namespace ltn {
@@ -66,6 +67,14 @@ template <class T, int DK, int VS> struct GradLds {
     static constexpr int S = 0, D = SB, K = 0, Q = KB, G = A, Y = A + GB, Z = A + 2 * GB, P = A, E = A + PB, BYTES = A + B;
 };
 
+// Value heads that share keys, bf16: one workgroup a unit (their sums take the registers), so K and Q stay in LDS and the next slab
+// is on its way, into a second buffer, while one is worked on.  P and E lie over the last slab's dO, dV and Z.
+template <class T, int DK, int VS> struct GradPipe {
+    typedef GradLds<T, DK, VS> L;
+    static constexpr int SLAB = L::BYTES, KQ = 2 * L::KB, VECS = KQ + 2 * SLAB, BYTES = VECS + 2 * 2048;
+    static_assert(SLAB % 1024 == 0 && L::A >= 2 * L::SB, "tiles of whole kilobytes");
+};
+
 // ONE: no other value head shares the keys.
 // All products are taken transposed: a lane's results are four features (or columns) of one token, 16 tok + lane % 16.  Of
 // dO Z^T and dV Z^T the waves of the first half take one, those of the second the other.
@@ -75,8 +84,9 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
     typedef GradLds<T, DK, VS> L;
     typedef typename El<T>::F F;
     constexpr int NT = DK / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[L::BYTES];
-    __shared__ __attribute__((aligned(16))) float vec[kVec];             // gam, end, beta, G in two parts
+    constexpr bool PIPE = !ONE && sizeof(T) == 2;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    __shared__ __attribute__((aligned(16))) float vec_of_one[PIPE ? 4 : kVec];       // gam, end, beta, G in two parts
     __shared__ __attribute__((aligned(16))) float row_of[2][kChunk], end_of[2][kChunk], col_of[kWaves][kChunk], part[kWaves];
     const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk, group = ONE ? 1 : a.H / a.Hk;
     DeltaSeq s;
@@ -88,10 +98,51 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
     const size_t key_row = ((size_t)s.row * a.Hk + hk) * a.N + s.first + t0;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     const unsigned base = lds_address(lds);
-    const RowReader<T, VS> row_v(base, r, lane);
-    const RowReader<T, kChunk> row_c(base, r, lane);
+    RowReader<T, VS> row_v(base, r, lane);
+    RowReader<T, kChunk> row_c(base, r, lane);
     ColReader<T, kChunk, false> col_c(base, lane);
-    ColReader<T, DK, false> col_k(base, lane);
+    ColReader<T, DK, false> col_k(base, lane), col_s(base, lane);        // of K and Q; of the states
+    typedef GradPipe<T, DK, VS> Pipe;
+    unsigned slab = base;                  // the slab's buffer; PIPE: behind K and Q, and the other one behind it
+    float* vec = PIPE ? (float*)(lds + Pipe::VECS) : vec_of_one;
+    auto fetch_slab = [&](int h, int v0, unsigned to, int n) {           // n: which of the heads, for its decays
+        const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first + t0, at = (size_t)slot * a.H + h;
+        TileFetch<T, VS, kWaves> g, y;
+        TileFetch<T, kChunk, kWaves, VS> z;
+        TileFetch<T, DK, kWaves, VS> st, d;
+        z.fetch((const char*)a.z + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, to + L::Z, w, lane);
+        y.fetch((const char*)a.dv + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, to + L::Y, w, lane);
+        g.fetch((const char*)a.d_o + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, to + L::G, w, lane);
+        st.fetch((const char*)a.s0 + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, to + L::S, w, lane);
+        d.fetch((const char*)a.ds + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, to + L::D, w, lane);
+        if constexpr (PIPE) {
+            if (v0 == 0 && w < 2) {        // 1280 bytes of decays and beta: 64 lanes of one wave, 16 of the next
+                const int piece = 64 * w + lane;
+                dma16(base + Pipe::VECS + (n & 1) * 2048 + w * 1024, piece < 80 ? (const char*)(a.vec + at * kVec) + piece * 16 : (const char*)kZeros);
+            }
+        } else {
+            if constexpr (sizeof(T) == 2) wait_dma<0>();
+            z.put(to + L::Z, w, lane);
+            y.put(to + L::Y, w, lane);
+            g.put(to + L::G, w, lane);
+            st.put(to + L::S, w, lane);
+            d.put(to + L::D, w, lane);
+        }
+    };
+    auto move_slab = [&](int by) {
+        slab += by;
+        row_v.move(by);
+        row_c.move(by);
+        col_c.move(by);
+        col_s.move(by);
+    };
+    if constexpr (PIPE) {
+        TileFetch<T, DK, kWaves> kt, qt;
+        kt.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::K, w, lane);
+        qt.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::Q, w, lane);
+        move_slab(Pipe::KQ);
+        fetch_slab(hk * group, 0, slab, 0);
+    }
 
     f32x4 dq[ONE ? 1 : NT], dk[ONE ? 1 : NT];
     if constexpr (!ONE)
@@ -101,7 +152,8 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
     for (int j = 0; j < group; ++j) {
         const int h = hk * group + j;
         const size_t val_row = ((size_t)s.row * a.H + h) * a.N + s.first + t0, at = (size_t)slot * a.H + h;
-        const float mine = threadIdx.x < kVec ? a.vec[at * kVec + threadIdx.x] : 0.f;
+        const float mine = !PIPE && threadIdx.x < kVec ? a.vec[at * kVec + threadIdx.x] : 0.f;
+        if constexpr (PIPE) vec = (float*)(lds + Pipe::VECS + (j & 1) * 2048);
         f32x4 pe[4], qs[NT], ks[NT], ke[NT];
 #pragma unroll
         for (int ct = 0; ct < 4; ++ct) pe[ct] = zero;
@@ -109,28 +161,24 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
         for (int t = 0; t < NT; ++t) qs[t] = ks[t] = ke[t] = zero;
         float sdot = 0.f;
         for (int v0 = 0; v0 < Dv; v0 += VS) {
-            TileFetch<T, VS, kWaves> g, y;
-            TileFetch<T, kChunk, kWaves, VS> z;
-            TileFetch<T, DK, kWaves, VS> st, d;
-            if (j || v0) __syncthreads();                                // the tiles' last readers are done
-            z.fetch((const char*)a.z + (at * Dv + v0) * (kChunk * sizeof(T)), kChunk * sizeof(T), VS, base + L::Z, w, lane);
-            y.fetch((const char*)a.dv + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, base + L::Y, w, lane);
-            g.fetch((const char*)a.d_o + (val_row * Dv + v0) * sizeof(T), Dv * sizeof(T), rows, base + L::G, w, lane);
-            st.fetch((const char*)a.s0 + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::S, w, lane);
-            d.fetch((const char*)a.ds + (at * Dv + v0) * (DK * sizeof(T)), DK * sizeof(T), VS, base + L::D, w, lane);
-            if constexpr (sizeof(T) == 2) wait_dma<0>();
-            z.put(base + L::Z, w, lane);
-            y.put(base + L::Y, w, lane);
-            g.put(base + L::G, w, lane);
-            st.put(base + L::S, w, lane);
-            d.put(base + L::D, w, lane);
-            if (v0 == 0 && threadIdx.x < kVec) vec[threadIdx.x] = mine;
-            __syncthreads();
+            if constexpr (PIPE) {
+                if (j || v0) move_slab(slab == base + Pipe::KQ ? Pipe::SLAB : -Pipe::SLAB);
+                wait_dma<0>();
+                __syncthreads();           // this slab is there, and the last one's readers (and those of P and E over it) are done
+                const bool more = v0 + VS < Dv;
+                if (more || j + 1 < group)
+                    fetch_slab(more ? h : h + 1, more ? v0 + VS : 0, slab == base + Pipe::KQ ? slab + Pipe::SLAB : slab - Pipe::SLAB, j + !more);
+            } else {
+                if (j || v0) __syncthreads();                            // the tiles' last readers are done
+                fetch_slab(h, v0, slab, 0);
+                if (v0 == 0 && threadIdx.x < kVec) vec[threadIdx.x] = mine;
+                __syncthreads();
+            }
             col_c.hide_all();
-            col_k.hide_all();
+            col_s.hide_all();
             for (int i = threadIdx.x; i < VS * DK / 8; i += kThreads) {  // (both tiles are laid out alike)
                 const int o = Tile<T, DK>::at(i / (DK / 8), i % (DK / 8) * 8);
-                sdot += dot8<T>(lds_frag<T>(base + L::S + o), lds_frag<T>(base + L::D + o));
+                sdot += dot8<T>(lds_frag<T>(slab + L::S + o), lds_frag<T>(slab + L::D + o));
             }
 #pragma unroll
             for (int kb = 0; kb < VS / 32; ++kb) {
@@ -142,17 +190,19 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
                 for (int ct = 0; ct < 4; ++ct) pe[ct] = mma(col_c.frag(L::Z, kb, ct), own, pe[ct]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const F sf = col_k.frag(L::S, kb, f0 + t), df = col_k.frag(L::D, kb, f0 + t);
+                    const F sf = col_s.frag(L::S, kb, f0 + t), df = col_s.frag(L::D, kb, f0 + t);
                     qs[t] = mma(sf, gf, qs[t]);
                     ks[t] = mma(sf, yf, ks[t]);
                     ke[t] = mma(df, zf, ke[t]);
                 }
             }
         }
-        __syncthreads();                   // the slab is read: K, Q, dP and E take its place
+        __syncthreads();                   // the slab is read: (K, Q,) dP and E take its place
         TileFetch<T, DK, kWaves> kt, qt;
-        kt.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::K, w, lane);
-        qt.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::Q, w, lane);
+        if constexpr (!PIPE) {
+            kt.fetch((const char*)a.k + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::K, w, lane);
+            qt.fetch((const char*)a.q + key_row * (DK * sizeof(T)), DK * sizeof(T), rows, base + L::Q, w, lane);
+        }
         {
             const float ghi = vec[3 * kChunk + r], glo = vec[4 * kChunk + r], side = hf ? -1.f : a.scale;
 #pragma unroll
@@ -167,7 +217,7 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
                     const float y = side * expf((ghi - chi[i]) + (glo - clo[i])) * pe[ct][i];
                     x[i] = r >= c + i + hf ? y : 0.f;
                 }
-                write4<T>(base + (hf ? L::E : L::P) + Tile<T, kChunk>::at(r, c), x * bc);
+                write4<T>(slab + (hf ? L::E : L::P) + Tile<T, kChunk>::at(r, c), x * bc);
             }
         }
         const float beta = vec[2 * kChunk + r], gam = vec[r], end = vec[kChunk + r];
@@ -177,9 +227,11 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
             ks[t] = times(ks[t], -gam);
             ke[t] = times(ke[t], end);
         }
-        if constexpr (sizeof(T) == 2) wait_dma<0>();
-        kt.put(base + L::K, w, lane);
-        qt.put(base + L::Q, w, lane);
+        if constexpr (!PIPE) {
+            if constexpr (sizeof(T) == 2) wait_dma<0>();
+            kt.put(base + L::K, w, lane);
+            qt.put(base + L::Q, w, lane);
+        }
         __syncthreads();
         float sum = 0.f, ends = 0.f;       // of token r: what its row gives dG; k . C
 #pragma unroll
@@ -284,11 +336,12 @@ void delta_grad_kernel(DeltaArgs a, int Dv) {
 
 template <class T, int DK, int VS>
 hipError_t launch_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((long long)a.slots * a.Hk)), dim3(kThreads), 0, stream, a, Dv);
-        return hipGetLastError();
-    };
-    return a.H == a.Hk ? launch(delta_grad_kernel<T, DK, VS, true>) : launch(delta_grad_kernel<T, DK, VS, false>);
+    constexpr int ALONE = GradLds<T, DK, VS>::BYTES, SHARED = sizeof(T) == 2 ? GradPipe<T, DK, VS>::BYTES : ALONE;
+    static_assert(SHARED <= 155 * 1024, "LDS");
+    const bool one = a.H == a.Hk;
+    hipLaunchKernelGGL((one ? delta_grad_kernel<T, DK, VS, true> : delta_grad_kernel<T, DK, VS, false>),
+                       dim3((unsigned)((long long)a.slots * a.Hk)), dim3(kThreads), one ? ALONE : SHARED, stream, a, Dv);
+    return hipGetLastError();
 }
 
 }  // namespace
