@@ -348,7 +348,7 @@ ltn_status ltn_attn_decode_steps_dkdv(const void* q, const void* k, const void* 
  *                 as it was.  Values are not read on the host; whatever they are, no access leaves the tensors (sequences
  *                 that they make overlap have undefined results).  seqs is not used without cu
  *   workspace   : device scratch of ltn_delta_workspace_bytes(..., call = 0) bytes
- * (Dk, Dv) in {64,128} x {64,128}; N <= 2^31 - 65, fewer than 2^22 sequences x value heads and 2^23 chunks x value heads
+ * (Dk, Dv) in {64,128} x {64,128}; N <= 2^31 - 65, fewer than 2^21 sequences x value heads and 2^23 chunks x value heads
  * (LTN_ERR_SHAPE).  fp32 tensors: fp32 arithmetic throughout; the order of a sum may depend on how many sequences and heads a
  * call has.  bf16 tensors: bf16 matrix products with fp32 sums; what enters the state enters in two bf16 parts, so that
  * kv_out is exact to about 4e-6 of its norm, not to a bf16 rounding; o is rounded to bf16.  An infinity or NaN in a token

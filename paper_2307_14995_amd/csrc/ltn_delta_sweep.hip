@@ -16,14 +16,14 @@
 //
 // fp32 (matrix products at a sixteenth of the bf16 rate, which bound it): while there are workgroups for no more than
 // half of the compute units, two waves share 16 columns, each with half of the features, and add their parts of K S and
-// Q S through LDS.  Two rows of 700 tokens, 8 heads of 64: forward 75 -> 60 us, the gradients' sweeps 53 -> 40 and 84 ->
-// 67.  (bf16 gains nothing from it: one prompt of 3001 tokens 116 us either way.)
+// Q S through LDS.  Two rows of 700 tokens, 8 heads of 64: forward 75 -> 59 us, the gradients' sweeps 53 -> 40 and 84 -> 66
+// by themselves.  (bf16 gains nothing from it: one prompt of 3001 tokens 116 us either way.)
 //
 // What bounds them, heads of 128 features: 256 or more workgroups, HBM (4 rows of 8192 tokens, 32 heads, bf16: forward 316
-// us at 4.6 TB/s, the gradients' two 290 and 375 at 4.9); fewer, a chunk's chain of dependent steps, 1.9 to 2.4 us: of the
+// us at 4.6 TB/s, the gradients' two 650 at 5.1); fewer, a chunk's chain of dependent steps, 1.9 to 2.8 us: of the
 // forward's 4500 cycles matrix products take 1660 and vector instructions 1990, which one wave a SIMD hardly overlaps
 // (asked to interleave them, the compiler ran out of registers: 128 us for 70), and LDS is busy 1580.  One prompt of 3001
-// tokens, 47 chunks, 91 us; 8 rows of 2048 tokens, 8 heads: 68, 61 and 76 us.
+// tokens, 47 chunks, 91 us; 8 rows of 2048 tokens, 8 heads: 68 us, and the gradients' two sweeps 90 together (61 and 76 alone).
 #include "ltn_delta.h"
 
 namespace ltn {
@@ -133,8 +133,7 @@ template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepFetch {
 
 // Forward.  SAVE: Z and the states before chunks are written, for the gradients, and O is not.
 template <class T, int DK, int KS, bool SAVE>
-__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
+__device__ __forceinline__ void forward_sweep(const DeltaArgs& a, int Dv, int per_chain, int wg) {
     constexpr bool BF = sizeof(T) == 2;
     static_assert(KS == 1 || !BF, "the waves that fetch take no part in the exchange");
     constexpr int COLS = 16 * W / KS, NT = DK / 16 / KS, NP = NT / 2, NO = 4 / KS;
@@ -143,7 +142,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];        // (of a size unknown to the compiler, which would else plan for one wave a SIMD and move accumulators to and fro)
 
     int chain, split;
-    map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
+    map_workgroup(wg, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
@@ -384,8 +383,7 @@ void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
 
 // Backward, from the last chunk to the first: dV and the derivatives of the states behind chunks.
 template <class T, int DK, int KS>
-__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
+__device__ __forceinline__ void backward_sweep(const DeltaArgs& a, int Dv, int per_chain, int wg) {
     constexpr bool BF = sizeof(T) == 2;
     static_assert(KS == 1 || !BF, "the waves that fetch take no part in the exchange");
     constexpr int COLS = 16 * W / KS, NT = DK / 16 / KS, NP = NT / 2;
@@ -394,7 +392,7 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
 
     int chain, split;
-    map_workgroup(blockIdx.x, per_chain, a.seqs * a.H, chain, split);
+    map_workgroup(wg, per_chain, a.seqs * a.H, chain, split);
     const int seq = chain / a.H, h = chain % a.H;
     const DeltaSeq s = delta_seq(a, seq);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, grp = lane >> 4;
@@ -557,34 +555,51 @@ void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
     }
 }
 
-template <class T, int DK, int KS, bool SAVE>
+template <class T, int DK, int KS>
+__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+void delta_fwd_kernel(DeltaArgs a, int Dv, int per_chain) {
+    forward_sweep<T, DK, KS, false>(a, Dv, per_chain, blockIdx.x);
+}
+
+// The gradients' two sweeps do not need each other: the first half of the workgroups go backward, which takes longer, and the
+// second half save the states.  Where chains are few, they have the units that one sweep alone would leave idle.
+template <class T, int DK, int KS>
+__global__ __launch_bounds__(kThreadsOf<T>) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+void delta_bwd_kernel(DeltaArgs a, int Dv, int per_chain) {
+    const int half = gridDim.x / 2, wg = blockIdx.x;
+    if (wg < half) backward_sweep<T, DK, KS>(a, Dv, per_chain, wg);
+    else forward_sweep<T, DK, KS, true>(a, Dv, per_chain, wg - half);
+}
+
+template <class T, int DK, int KS>
 hipError_t launch_fwd_ks(const DeltaArgs& a, int Dv, hipStream_t stream) {
-    constexpr int COLS = 16 * W / KS, LDS = SweepLds<T, DK, COLS, !SAVE, true>::ALL + (KS > 1 ? W * Swap<SAVE>::BYTES : 0);
+    constexpr int COLS = 16 * W / KS, LDS = SweepLds<T, DK, COLS, true, true>::ALL + (KS > 1 ? W * Swap<false>::BYTES : 0);
     static_assert(LDS <= 160 * 1024, "LDS");
-    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, KS, SAVE>), dim3((unsigned)((long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
+    hipLaunchKernelGGL((delta_fwd_kernel<T, DK, KS>), dim3((unsigned)((long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
     return hipGetLastError();
 }
 template <class T, int DK, int KS>
 hipError_t launch_bwd_ks(const DeltaArgs& a, int Dv, hipStream_t stream) {
     constexpr int COLS = 16 * W / KS, LDS = SweepLds<T, DK, COLS, true, false>::ALL + W * (Turn<T>::BYTES + (KS > 1 ? Swap<true>::BYTES : 0));
-    static_assert(LDS <= 160 * 1024, "LDS");
-    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, KS>), dim3((unsigned)((long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
+    static_assert(LDS <= 160 * 1024 && LDS >= SweepLds<T, DK, COLS, false, true>::ALL + (KS > 1 ? W * Swap<true>::BYTES : 0), "LDS");
+    hipLaunchKernelGGL((delta_bwd_kernel<T, DK, KS>), dim3((unsigned)(2 * (long long)a.seqs * a.H * (Dv / COLS))), dim3(kThreadsOf<T>), LDS, stream, a, Dv, Dv / COLS);
     return hipGetLastError();
 }
-// fp32, while each of twice as many workgroups has a compute unit of its own: two waves share 16 columns.  Forward of
-// sequences of 700 tokens, heads of 128 features, a wave a column and half a wave: 32 workgroups 123 and 94 us, 128 (the
-// last that share) 140 and 111, 256 164 and 212, 512 333 and 437.
-bool shared_columns(const DeltaArgs& a, int Dv) { return (long long)a.seqs * a.H * (Dv / (16 * W)) * 2 <= 256; }
-template <class T, int DK, bool SAVE>
+// fp32, while each of twice as many workgroups (of both sweeps, in the gradients) has a compute unit of its own: two waves
+// share 16 columns.  Forward of sequences of 700 tokens, heads of 128 features, a wave a column and half a wave: 32 workgroups
+// 123 and 94 us, 128 (the last that share) 140 and 111, 256 164 and 212, 512 333 and 437.  Gradients, whole calls: 2 x 16
+// of 64 features 112 and 95 us, 2 x 128 214 and 233; 2 x 32 of 128 features 192 and 147, 2 x 128 299 and 305.
+bool shared_columns(const DeltaArgs& a, int Dv, int sweeps) { return (long long)a.seqs * a.H * (Dv / (16 * W)) * 2 * sweeps <= 256; }
+template <class T, int DK>
 hipError_t launch_fwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
     if constexpr (sizeof(T) == 4)
-        if (shared_columns(a, Dv)) return launch_fwd_ks<T, DK, 2, SAVE>(a, Dv, stream);
-    return launch_fwd_ks<T, DK, 1, SAVE>(a, Dv, stream);
+        if (shared_columns(a, Dv, 1)) return launch_fwd_ks<T, DK, 2>(a, Dv, stream);
+    return launch_fwd_ks<T, DK, 1>(a, Dv, stream);
 }
 template <class T, int DK>
 hipError_t launch_bwd_t(const DeltaArgs& a, int Dv, hipStream_t stream) {
     if constexpr (sizeof(T) == 4)
-        if (shared_columns(a, Dv)) return launch_bwd_ks<T, DK, 2>(a, Dv, stream);
+        if (shared_columns(a, Dv, 2)) return launch_bwd_ks<T, DK, 2>(a, Dv, stream);
     return launch_bwd_ks<T, DK, 1>(a, Dv, stream);
 }
 
@@ -595,15 +610,12 @@ hipError_t launch_delta_fwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hip
         const hipError_t e = launch_delta_prepare(a, Dk, is_bf16, stream);
         if (e != hipSuccess) return e;
     }
-    if (Dk == 64) return is_bf16 ? launch_fwd_t<__bf16, 64, false>(a, Dv, stream) : launch_fwd_t<float, 64, false>(a, Dv, stream);
-    return is_bf16 ? launch_fwd_t<__bf16, 128, false>(a, Dv, stream) : launch_fwd_t<float, 128, false>(a, Dv, stream);
+    if (Dk == 64) return is_bf16 ? launch_fwd_t<__bf16, 64>(a, Dv, stream) : launch_fwd_t<float, 64>(a, Dv, stream);
+    return is_bf16 ? launch_fwd_t<__bf16, 128>(a, Dv, stream) : launch_fwd_t<float, 128>(a, Dv, stream);
 }
 
 hipError_t launch_delta_bwd(const DeltaArgs& a, int Dk, int Dv, int is_bf16, hipStream_t stream) {
     hipError_t e = launch_delta_prepare(a, Dk, is_bf16, stream);
-    if (e != hipSuccess) return e;
-    if (Dk == 64) e = is_bf16 ? launch_fwd_t<__bf16, 64, true>(a, Dv, stream) : launch_fwd_t<float, 64, true>(a, Dv, stream);
-    else e = is_bf16 ? launch_fwd_t<__bf16, 128, true>(a, Dv, stream) : launch_fwd_t<float, 128, true>(a, Dv, stream);
     if (e != hipSuccess) return e;
     if (Dk == 64) e = is_bf16 ? launch_bwd_t<__bf16, 64>(a, Dv, stream) : launch_bwd_t<float, 64>(a, Dv, stream);
     else e = is_bf16 ? launch_bwd_t<__bf16, 128>(a, Dv, stream) : launch_bwd_t<float, 128>(a, Dv, stream);

@@ -37,8 +37,8 @@ ltn_status check_delta(int Bt, int Hk, int H, long long N, int Dk, int Dv, bool 
     return LTN_OK;
 }
 
-// A launch has at most 2^32 threads in its grid: the sweeps up to 1024 a chain, "grad" 512 a chunk and head.
-bool launches(const DeltaDims& d, int H) { return d.chains < (1 << 22) && d.slots * H < (1 << 23); }
+// A launch has less than 2^32 threads in its grid: the sweeps up to 2048 a chain, "grad" 512 a chunk and head.
+bool launches(const DeltaDims& d, int H) { return d.chains < (1 << 21) && d.slots * H < (1 << 23); }
 
 // Hands out the workspace's arrays; returns its size.
 size_t lay_out(ltn::DeltaArgs& a, char* base, int Dk, int Dv, bool bf16, bool bwd) {
