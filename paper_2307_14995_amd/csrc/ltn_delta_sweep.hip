@@ -2,7 +2,8 @@
 // state: all Dk rows of them stay in its accumulators from the first chunk to the last, and as the columns of S, X, Z, U,
 // O (and of dS, dU, dV) are independent, no wave waits for another's result.  The state's rows and the tokens are dealt
 // to the accumulators' rows so (paired()) that one product's results are, lane by lane, the next one's right operand:
-// nothing between the products passes through LDS.  What the four waves share are the chunk's tiles, the left operands.
+// nothing between the products passes through LDS (but in fp32, see below).  What the four waves share are the chunk's
+// tiles, the left operands.
 //
 // bf16: the tiles of the next chunk are fetched into a second buffer by four waves that do nothing else.  (A wave's next
 // load waits until the memory path has taken its last one, 57 to 90 cycles; the waves that compute spent two thirds of a
@@ -77,7 +78,7 @@ template <class T> __device__ __forceinline__ void fence() {
 // What a wave hands the one that has the other features of its columns: K S (or K dS), and O's other two row tiles.
 template <bool SAVE> struct Swap { static constexpr int BYTES = (SAVE ? 4 : 6) * 1024; };
 
-// One chunk's tiles in LDS.  FWD: K, T', V and, where O is wanted, T's second part (bf16), Q and P.  Backward: K, Q, T', P, dO.
+// One chunk's tiles in LDS.  FWD: K, T', V and, where O is wanted, the second part of T' (bf16), Q and P.  Backward: K, Q, T', P, dO.
 template <class T, int DK, int COLS, bool FULL, bool FWD> struct SweepLds {
     static constexpr int K = 0, T1 = K + Tile<T, DK>::BYTES, V = T1 + Tile<T, kChunk>::BYTES, VEC = V + Tile<T, COLS>::BYTES,
                          T2 = VEC + 1024, Q = T2 + (FWD && FULL && sizeof(T) == 2 ? Tile<T, kChunk>::BYTES : 0),
